@@ -67,6 +67,9 @@ typedef enum {
 #define APC_MAX_INST 256      /* largest number of model instances */
 #define APC_MAX_SHARDS 64     /* largest number of row shards apc_merge_shards merges */
 #define APC_MAX_ROUTED_BATCH 16384  /* largest batch of apc_assign_routed / apc_assign_planned */
+#define APC_MAX_NORM_D 32768  /* longest row apc_norm_rows takes */
+#define APC_MAX_HEAD_DIM 256  /* largest head of a key-value cache */
+#define APC_MAX_PAGE 1024     /* most tokens of a key-value page */
 
 /* opaque, immutable after build */
 typedef struct apc_cache apc_cache;
@@ -408,6 +411,126 @@ apc_status apc_gather_latents_at_level(const apc_cache* c, const int32_t* top_id
 apc_status apc_merge_shards(const float* scores, const int32_t* idx, int32_t g, int32_t b, int32_t k_in,
                             const int32_t* offsets /* host */, int32_t k, float* out_score, int32_t* out_idx,
                             void* stream);
+
+/*
+ * Operators of the prompt model (not a step of the paper, which takes prompt
+ * embeddings as given: what a dispatcher that also runs the text model needs
+ * to make them, one new token of every prompt at a time).  Rows of the new
+ * tokens are normed (apc_norm_rows), their keys and values go into a paged
+ * cache (apc_kv_write), attention reads it (apc_attend), and the last norm
+ * leaves e4m3 rows with their scales, the form in which apc_match_batch takes
+ * queries.  These calls take strides in elements, so that views of wider rows
+ * (a fused product's output) need no copy; their buffers need only the
+ * alignment of their element type, except where 16 bytes are asked for.
+ */
+
+/*
+ * Root-mean-square norm of n rows of d elements, with the residual's addition
+ * before it:
+ *     h = x + res,   y = h / sqrt(mean(h^2) + eps) * weight,
+ * in float32 throughout, each output rounded once (nearest-even).
+ * dt          type of x, res, weight and sum: APC_F32, APC_F16 or APC_BF16.
+ * out_dt      dt, or APC_E4M3: per row the scale s = amax / 448 of y and the
+ *             codes of y / s, as apc_quantize_rows makes them.
+ * x, res      rows at strides ld_x, ld_res (>= d) elements; res NULL = no
+ *             residual (then sum must be NULL too).
+ * weight      d elements, or NULL = ones.
+ * sum         (nullable) h, at stride ld_sum; may be x's or res's own rows
+ *             (same address and stride), to update the residual in place.
+ * out         at stride ld_out; must not overlap the inputs, except that with
+ *             out_dt = dt it may be x's or res's own rows when sum is not the
+ *             same rows.
+ * out_scale   n float32 (APC_E4M3 only, else NULL).
+ * eps         finite, >= 0.  A row whose float32 sum of squares overflows
+ *             gives zeros; a zero row with eps = 0 gives NaN.
+ * 1 <= d <= APC_MAX_NORM_D.  n = 0 is a no-op.  Errors: APC_E_ARG,
+ * APC_E_DTYPE.  Asynchronous on stream.
+ */
+apc_status apc_norm_rows(apc_dtype dt, apc_dtype out_dt, int64_t n, int32_t d, const void* x, int64_t ld_x,
+                         const void* res, int64_t ld_res, const void* weight, float eps, void* sum, int64_t ld_sum,
+                         void* out, int64_t ld_out, float* out_scale, void* stream);
+
+/*
+ * Paged key-value cache: a description of the caller's buffers, passed by
+ * address (host).  Page p holds `page` tokens of every head; token t of page p
+ * is slot p * page + t.  Keys and values of head h of that token are the d
+ * elements at ((p * heads + h) * page + t) * d of k and of v; for APC_E4M3 an
+ * element's value is code * scale with the scale at (p * heads + h) * page + t
+ * of k_scale and of v_scale.
+ */
+typedef struct {
+    apc_dtype dt;        /* APC_F16, APC_BF16 or APC_E4M3 */
+    int32_t heads;       /* key-value heads, >= 1 */
+    int32_t d;           /* elements per head: a multiple of 16, <= APC_MAX_HEAD_DIM */
+    int32_t page;        /* tokens per page: a power of two, 16 <= page <= APC_MAX_PAGE */
+    int64_t n_pages;     /* n_pages * page < 2^31 */
+    void* k;             /* device, 16-byte aligned */
+    void* v;
+    float* k_scale;      /* device, 16-byte aligned (APC_E4M3 only, else NULL) */
+    float* v_scale;
+} apc_kv;
+
+/*
+ * Writes the keys and values of t tokens into the cache, converted as they
+ * are written: rounded to nearest-even (16-bit caches) or quantised per token
+ * and head as apc_quantize_rows quantises a row (e4m3).
+ * dt          type of k and v: APC_F32, APC_F16 or APC_BF16.
+ * k, v        t x heads x d: token i's head h at i * tok + h * head elements
+ *             (strides k_tok, k_head, v_tok, v_head >= 0; d elements contiguous).
+ * slots       t int32 (device): the slot of each token; a value outside the
+ *             cache's slots (-1 for padding) writes nothing.  Two tokens with
+ *             one slot leave either's rows there.
+ * t = 0 is a no-op.  Errors: APC_E_ARG, APC_E_DTYPE.  Asynchronous on stream.
+ */
+apc_status apc_kv_write(const apc_kv* c /* host */, apc_dtype dt, int64_t t, const void* k, int64_t k_tok,
+                        int64_t k_head, const void* v, int64_t v_tok, int64_t v_head, const int32_t* slots,
+                        void* stream);
+
+/*
+ * Reads t slots back as rows of type dt (APC_F32, APC_F16 or APC_BF16): the
+ * stored values (code * scale, one float32 product), rounded to nearest-even.
+ * A slot outside the cache's gives zeros.  Arguments as for apc_kv_write, k
+ * and v being outputs.
+ */
+apc_status apc_kv_read(const apc_kv* c /* host */, apc_dtype dt, int64_t t, const int32_t* slots, void* k,
+                       int64_t k_tok, int64_t k_head, void* v, int64_t v_tok, int64_t v_head, void* stream);
+
+/* Workspace bytes apc_attend needs for b sequences of q_heads query heads and
+   page tables of max_pages entries.  Never falls as b or max_pages grows. */
+apc_status apc_attend_workspace(const apc_kv* c /* host */, int32_t b, int32_t q_heads, int32_t max_pages,
+                                size_t* bytes /* host */);
+
+/*
+ * Attention of one new token of each of b sequences over the sequence's
+ * cached tokens.  For sequence i, query head a and its key-value head
+ * h = a / (q_heads / heads):
+ *     s_j = scale * <q, k_j>,  o = sum_j exp(s_j) v_j / sum_j exp(s_j),
+ *     lse = ln sum_j exp(s_j),
+ * over the tokens j in [max(0, len - window), len) (window = 0: all), len =
+ * lengths[i] cut to 0..max_pages * page, whose page entry is in 0..n_pages-1
+ * (others are left out; the new token's own key and value are in the cache,
+ * written before).  No token left: o = 0, lse = -inf.  Nothing outside those
+ * tokens reaches the result, whatever it holds.  Scores, the running maximum
+ * and sum and the output's sums are float32; the weights of the values enter
+ * the matrix product as two 16-bit parts each.
+ * dt          type of q and out: the cache's, or APC_F16 / APC_BF16 where the
+ *             cache is APC_E4M3.
+ * q, out      sequence i's head a at i * row + a * head elements (strides
+ *             q_row, q_head, out_row, out_head >= 0; d contiguous).
+ * q_heads     a multiple of the cache's heads.
+ * pages       b x max_pages int32 page numbers at row stride ld_pages.
+ * lengths     b int32.
+ * window      >= 0.   scale: finite.
+ * lse         b x q_heads float32, or NULL.
+ * ws          workspace of at least apc_attend_workspace() bytes (16-byte
+ *             aligned); nothing in it needs to start at zero.
+ * b = 0 is a no-op.  Errors: APC_E_ARG, APC_E_DTYPE, APC_E_WORKSPACE.
+ * Asynchronous on stream.
+ */
+apc_status apc_attend(const apc_kv* c /* host */, apc_dtype dt, const void* q, int64_t q_row, int64_t q_head,
+                      int32_t b, int32_t q_heads, const int32_t* pages, int32_t max_pages, int64_t ld_pages,
+                      const int32_t* lengths, int32_t window, float scale, void* out, int64_t out_row,
+                      int64_t out_head, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Measurement hook (for benchmarks and profilers, not for the method):

@@ -547,3 +547,87 @@ def validate_rows(dtype: str, rows: np.ndarray, scale=None) -> np.ndarray:
         s = np.asarray(scale, dtype=np.float32)
         flags |= np.where(np.isfinite(s) & (s > 0), 0, BAD_SCALE)
     return flags.astype(np.uint8)
+
+
+# ---- operators of the prompt model (float64, from the formulas) ----
+
+def norm_rows(x, res, weight, eps: float):
+    """(y, h) in float64 of rows x (+ res): h = x + res, y = h / sqrt(mean(h^2) + eps) * weight."""
+    h = np.asarray(x, dtype=np.float64)
+    if res is not None:
+        h = h + np.asarray(res, dtype=np.float64)
+    with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+        y = h / np.sqrt((h * h).mean(axis=1, keepdims=True) + float(eps))
+    if weight is not None:
+        y = y * np.asarray(weight, dtype=np.float64)
+    return y, h
+
+
+def kv_write(dtype: str, pool: np.ndarray, scale, x: np.ndarray, slots):
+    """Writes rows x (t x heads x d float32) into pool (n_pages x heads x page x d, stored elements) and scale in
+    place; later tokens win where two share a slot."""
+    n_pages, heads, page, _ = pool.shape
+    for i, s in enumerate(np.asarray(slots, dtype=np.int64)):
+        if s < 0 or s >= n_pages * page:
+            continue
+        rows, sc = quantize_rows(dtype, x[i])
+        pool[s // page, :, s % page] = rows
+        if scale is not None:
+            scale[s // page, :, s % page] = sc
+
+
+def kv_read(dtype: str, pool: np.ndarray, scale, slots, out: str):
+    """t x heads x d rows of the slots: float32 values code * scale (rounded to float32), in the type `out`."""
+    n_pages, heads, page, d = pool.shape
+    rows = np.zeros((len(slots), heads, d), dtype=np.float32)
+    for i, s in enumerate(np.asarray(slots, dtype=np.int64)):
+        if s < 0 or s >= n_pages * page:
+            continue
+        v = kv_values(dtype, pool[s // page, :, s % page]).astype(np.float32)
+        rows[i] = v if scale is None else v * scale[s // page, :, s % page][:, None].astype(np.float32)
+    if out == "f32":
+        return rows
+    return quantize_rows(out, rows.reshape(-1, d))[0].reshape(rows.shape)
+
+
+def kv_values(dtype: str, stored: np.ndarray) -> np.ndarray:
+    """float64 values of stored elements, scales left out."""
+    if dtype == "f16":
+        return stored.view(np.float16).astype(np.float64)
+    if dtype == "bf16":
+        return (stored.view(np.uint16).astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+    return e4m3_values()[stored.view(np.uint8)]
+
+
+def attend(dtype: str, q, k: np.ndarray, v: np.ndarray, k_scale, v_scale, pages, lengths, scale: float, window: int = 0):
+    """(out, lse, spread, top) in float64.  q: b x q_heads x d values.  spread = sum_j p_j |v_j| / sum_j p_j per
+    output element and top = the largest scale * sum_e |q_e k_je| per query head: what rounding errors scale with."""
+    n_pages, heads, page, d = k.shape
+    q = np.asarray(q, dtype=np.float64)
+    b, hq, _ = q.shape
+    group = hq // heads
+    out = np.zeros((b, hq, d))
+    spread = np.zeros((b, hq, d))
+    lse = np.full((b, hq), -np.inf)
+    top = np.zeros((b, hq))
+    for i in range(b):
+        n = min(max(int(lengths[i]), 0), pages.shape[1] * page)
+        j = np.arange(max(0, n - window) if window else 0, n)
+        p = pages[i][j // page].astype(np.int64) if n else np.zeros(0, np.int64)
+        j, p = j[(p >= 0) & (p < n_pages)], p[(p >= 0) & (p < n_pages)]
+        if j.size == 0:
+            continue
+        for h in range(heads):
+            kk, vv = kv_values(dtype, k[p, h, j % page]), kv_values(dtype, v[p, h, j % page])
+            if k_scale is not None:
+                kk = kk * k_scale[p, h, j % page].astype(np.float64)[:, None]
+                vv = vv * v_scale[p, h, j % page].astype(np.float64)[:, None]
+            for a in range(h * group, (h + 1) * group):
+                s = scale * (kk @ q[i, a])
+                m = s.max()
+                w = np.exp(s - m)
+                lse[i, a] = m + np.log(w.sum())
+                out[i, a] = w @ vv / w.sum()
+                spread[i, a] = w @ np.abs(vv) / w.sum()
+                top[i, a] = abs(scale) * (np.abs(kk) @ np.abs(q[i, a])).max()
+    return out, lse, spread, top

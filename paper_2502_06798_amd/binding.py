@@ -33,6 +33,13 @@ class ApcError(RuntimeError):
         super().__init__(f"{self.name}: {msg}")
 
 
+class _KvStruct(ctypes.Structure):
+    """apc_kv of include/apc.h."""
+    _fields_ = [("dt", ctypes.c_int), ("heads", ctypes.c_int32), ("d", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("n_pages", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -89,6 +96,18 @@ def load() -> ctypes.CDLL:
     L.apc_merge_shards.restype = st
     L.apc_gather_latents.argtypes = [vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp]
     L.apc_gather_latents.restype = st
+    f32, kv = ctypes.c_float, ctypes.POINTER(_KvStruct)
+    L.apc_norm_rows.argtypes = [ctypes.c_int, ctypes.c_int, i64, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, vp]
+    L.apc_norm_rows.restype = st
+    L.apc_kv_write.argtypes = [kv, ctypes.c_int, i64, vp, i64, i64, vp, i64, i64, vp, vp]
+    L.apc_kv_write.restype = st
+    L.apc_kv_read.argtypes = [kv, ctypes.c_int, i64, vp, vp, i64, i64, vp, i64, i64, vp]
+    L.apc_kv_read.restype = st
+    L.apc_attend_workspace.argtypes = [kv, i32, i32, i32, ctypes.POINTER(sz)]
+    L.apc_attend_workspace.restype = st
+    L.apc_attend.argtypes = [kv, ctypes.c_int, vp, i64, i64, i32, i32, vp, i32, i64, vp, i32, f32, vp, i64, i64, vp, vp,
+                             sz, vp]
+    L.apc_attend.restype = st
     L.apc_set_kernel_events.argtypes = [vp, vp]
     L.apc_set_kernel_events.restype = st
     L.apc_status_str.argtypes = [ctypes.c_int]
@@ -348,3 +367,123 @@ def apc_merge_shards(scores: torch.Tensor, idx: torch.Tensor, g: int, b: int, k_
         raise ValueError("apc_merge_shards: need one offset per shard")
     _check(load().apc_merge_shards(_ptr(scores), _ptr(idx), g, b, k_in, _hp(off), k, _ptr(out_score),
                                    _ptr(out_idx), _stream(stream)))
+
+
+# ---- operators of the prompt model ----
+
+def _rows(t: torch.Tensor, what: str):
+    """Address of a device tensor whose last axis is contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the last axis must be contiguous")
+    return t.data_ptr()
+
+
+def _like(t: torch.Tensor, what: str, shape, dtype):
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
+
+
+def apc_norm_rows(x: torch.Tensor, out: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                  res: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+                  out_scale: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None):
+    """Root-mean-square norm of the rows of x (+ res): n x d tensors whose rows may be strided.  out is of x's type
+    or float8_e4m3fn (then out_scale holds a float32 scale per row); sum_out, if given, gets x + res."""
+    if x.dim() != 2 or x.dtype not in DTYPE_OF or out.dtype not in DTYPE_OF:
+        raise ValueError("x and out must be 2-D float32/float16/bfloat16 tensors (out: float8_e4m3fn too)")
+    n, d = x.shape
+    _like(out, "out", x.shape, out.dtype)
+    if weight is not None:
+        _like(weight, "weight", (d,), x.dtype)
+    for t, what in ((res, "res"), (sum_out, "sum_out")):
+        if t is not None:
+            _like(t, what, x.shape, x.dtype)
+    if out_scale is not None:
+        _like(out_scale, "out_scale", (n,), torch.float32)
+    _check(load().apc_norm_rows(
+        DTYPE_OF[x.dtype], DTYPE_OF[out.dtype], n, d, _rows(x, "x"), _ld(x),
+        None if res is None else _rows(res, "res"), 0 if res is None else _ld(res), _ptr(weight), eps,
+        None if sum_out is None else _rows(sum_out, "sum_out"), 0 if sum_out is None else _ld(sum_out),
+        _rows(out, "out"), _ld(out), _ptr(out_scale), _stream(stream)))
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row stride of a 2-D tensor (of one row: its width, whatever stride torch reports)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class KvCache:
+    """Paged key-value cache over caller tensors: k and v n_pages x heads x page x d (float16, bfloat16 or
+    float8_e4m3fn), k_scale and v_scale n_pages x heads x page float32 (float8_e4m3fn only).  Keeps the tensors
+    alive; slot p * page + t is token t of page p."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        if k.dim() != 4 or k.dtype not in DTYPE_OF:
+            raise ValueError("k must be an n_pages x heads x page x d float16/bfloat16/float8_e4m3fn tensor")
+        _like(v, "v", k.shape, k.dtype)
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t is not None:
+                _like(t, what, k.shape[:3], torch.float32)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.heads, self.page, self.d = k.shape
+        self.struct = _KvStruct(DTYPE_OF[k.dtype], self.heads, self.d, self.page, self.n_pages, _ptr(k), _ptr(v),
+                                _ptr(k_scale), _ptr(v_scale))
+        self.ref = ctypes.byref(self.struct)
+
+
+def _kv_rows(c: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
+    t = slots.shape[0]
+    if slots.dim() != 1 or slots.dtype != torch.int32:
+        raise ValueError("slots must be a 1-D int32 tensor")
+    if k.dtype not in DTYPE_OF:
+        raise ValueError("k and v must be float32/float16/bfloat16 tensors")
+    _like(k, "k", (t, c.heads, c.d), k.dtype)
+    _like(v, "v", (t, c.heads, c.d), k.dtype)
+    return DTYPE_OF[k.dtype], t
+
+
+def apc_kv_write(c: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
+    """Keys and values (t x heads x d, tokens and heads strided as they come) into the cache's slots."""
+    dt, t = _kv_rows(c, k, v, slots)
+    _check(load().apc_kv_write(c.ref, dt, t, _rows(k, "k"), k.stride(0), k.stride(1), _rows(v, "v"), v.stride(0),
+                               v.stride(1), _ptr(slots), _stream(stream)))
+
+
+def apc_kv_read(c: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None):
+    """The slots' keys and values into k and v (t x heads x d)."""
+    dt, t = _kv_rows(c, k, v, slots)
+    _check(load().apc_kv_read(c.ref, dt, t, _ptr(slots), _rows(k, "k"), k.stride(0), k.stride(1), _rows(v, "v"),
+                              v.stride(0), v.stride(1), _stream(stream)))
+
+
+def apc_attend_workspace(c: KvCache, b: int, q_heads: int, max_pages: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load().apc_attend_workspace(c.ref, b, q_heads, max_pages, ctypes.byref(n)))
+    return n.value
+
+
+def attend_workspace_tensor(c: KvCache, b: int, q_heads: int, max_pages: int, device=None) -> torch.Tensor:
+    """Device buffer of apc_attend_workspace() bytes (torch allocations are 256-byte aligned)."""
+    return torch.empty(max(apc_attend_workspace(c, b, q_heads, max_pages), 256), dtype=torch.uint8,
+                       device=device or "cuda")
+
+
+def apc_attend(c: KvCache, q: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor, scale: float,
+               out: torch.Tensor, ws: torch.Tensor, lse: Optional[torch.Tensor] = None, window: int = 0, stream=None):
+    """Attention of one new token per sequence: q and out b x q_heads x d, pages b x max_pages int32 (page numbers of
+    each sequence, rows may be strided), lengths b int32, lse b x q_heads float32 or None."""
+    if q.dim() != 3 or q.dtype not in DTYPE_OF or pages.dim() != 2 or pages.dtype != torch.int32:
+        raise ValueError("q must be a b x q_heads x d float16/bfloat16 tensor and pages a b x max_pages int32 tensor")
+    b, q_heads, d = q.shape
+    _like(out, "out", (b, q_heads, c.d), q.dtype)
+    if d != c.d or pages.shape[0] != b:
+        raise ValueError(f"q has {d} elements a head and the cache {c.d}; pages has {pages.shape[0]} rows for {b}")
+    _like(lengths, "lengths", (b,), torch.int32)
+    if lse is not None:
+        _like(lse, "lse", (b, q_heads), torch.float32)
+    _check(load().apc_attend(
+        c.ref, DTYPE_OF[q.dtype], _rows(q, "q"), q.stride(0), q.stride(1), b, q_heads, _rows(pages, "pages"),
+        pages.shape[1], _ld(pages), _ptr(lengths), window, scale, _rows(out, "out"), out.stride(0), out.stride(1),
+        _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))

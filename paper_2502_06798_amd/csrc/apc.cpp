@@ -92,6 +92,54 @@ apc_status check_device(const char* who, const apc_cache* c)
     return APC_OK;
 }
 
+bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+bool float_dtype(int dt) { return dt == APC_F32 || dt == APC_F16 || dt == APC_BF16; }
+
+// The description of a key-value cache.
+apc_status check_kv(const char* who, const apc_kv* c)
+{
+    if (!c) return fail(APC_E_ARG, "%s: NULL cache", who);
+    if (c->dt != APC_F16 && c->dt != APC_BF16 && c->dt != APC_E4M3)
+        return fail(APC_E_DTYPE, "%s: a key-value cache is f16, bf16 or e4m3 (got %d)", who, (int)c->dt);
+    if (c->heads < 1 || c->d < 16 || c->d > APC_MAX_HEAD_DIM || c->d % 16 != 0)
+        return fail(APC_E_ARG, "%s: need heads >= 1 and d a multiple of 16 up to %d (heads=%d d=%d)", who,
+                    APC_MAX_HEAD_DIM, c->heads, c->d);
+    if (c->page < 16 || c->page > APC_MAX_PAGE || (c->page & (c->page - 1)) != 0)
+        return fail(APC_E_ARG, "%s: page must be a power of two from 16 to %d (page=%d)", who, APC_MAX_PAGE, c->page);
+    if (c->n_pages < 0 || c->n_pages > INT32_MAX / c->page)
+        return fail(APC_E_ARG, "%s: need 0 <= n_pages * page < 2^31 (n_pages=%lld)", who, (long long)c->n_pages);
+    if (c->n_pages > 0) {
+        if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v))
+            return fail(APC_E_ARG, "%s: k and v must be non-NULL 16-byte aligned device pointers", who);
+        const bool scaled = c->dt == APC_E4M3;
+        if (scaled != (c->k_scale != nullptr) || scaled != (c->v_scale != nullptr))
+            return fail(APC_E_ARG, "%s: k_scale and v_scale are required for e4m3 and only for e4m3", who);
+        if (scaled && (!aligned16(c->k_scale) || !aligned16(c->v_scale)))
+            return fail(APC_E_ARG, "%s: k_scale and v_scale must be 16-byte aligned", who);
+    }
+    return APC_OK;
+}
+
+apc_status kv_rows(const char* who, bool write, const apc_kv* c, apc_dtype dt, int64_t t, const void* k, int64_t k_tok,
+                   int64_t k_head, const void* v, int64_t v_tok, int64_t v_head, const int32_t* slots, void* stream)
+{
+    if (apc_status st = check_kv(who, c)) return st;
+    if (!float_dtype(dt)) return fail(APC_E_DTYPE, "%s: rows are f32, f16 or bf16 (got %d)", who, (int)dt);
+    // one workgroup holds at least four rows, and a grid has fewer than 2^31 workgroups
+    if (t < 0 || t > (int64_t)INT32_MAX / c->heads)
+        return fail(APC_E_ARG, "%s: need 0 <= t * heads < 2^31 (t=%lld)", who, (long long)t);
+    if (k_tok < 0 || k_head < 0 || v_tok < 0 || v_head < 0) return fail(APC_E_ARG, "%s: negative stride", who);
+    if (t == 0) return ok();
+    const int e = apc::elem_bytes(dt);
+    if (!k || !v || !slots || !aligned_to(k, e) || !aligned_to(v, e) || !aligned_to(slots, 4))
+        return fail(APC_E_ARG, "%s: k, v and slots must be device pointers aligned to their elements", who);
+    const apc::KvRows a{const_cast<void*>(k), const_cast<void*>(v), slots, t, k_tok, k_head, v_tok, v_head};
+    hipError_t err = apc::launch_kv_rows(write, dt, *c, a, static_cast<hipStream_t>(stream));
+    if (err != hipSuccess) return hip_fail(err, who);
+    return ok();
+}
+
 }  // namespace
 
 extern "C" {
@@ -633,6 +681,93 @@ apc_status apc_gather_latents_at_level(const apc_cache* c, const int32_t* top_id
 {
     return gather_impl("apc_gather_latents_at_level", c, top_idx, ld, b, out_level, out_inst, out_slot, n_inst,
                        slots_per_inst, levels_per_slot, batch_latents, hit, stream);
+}
+
+apc_status apc_norm_rows(apc_dtype dt, apc_dtype out_dt, int64_t n, int32_t d, const void* x, int64_t ld_x,
+                         const void* res, int64_t ld_res, const void* weight, float eps, void* sum, int64_t ld_sum,
+                         void* out, int64_t ld_out, float* out_scale, void* stream)
+{
+    if (!float_dtype(dt)) return fail(APC_E_DTYPE, "apc_norm_rows: rows are f32, f16 or bf16 (got %d)", (int)dt);
+    if (out_dt != dt && out_dt != APC_E4M3)
+        return fail(APC_E_DTYPE, "apc_norm_rows: the output is of the rows' type or e4m3 (got %d)", (int)out_dt);
+    if (n < 0 || n > INT32_MAX || d < 1 || d > APC_MAX_NORM_D)
+        return fail(APC_E_ARG, "apc_norm_rows: need 0 <= n < 2^31 and 1 <= d <= %d (n=%lld d=%d)", APC_MAX_NORM_D,
+                    (long long)n, d);
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(APC_E_ARG, "apc_norm_rows: eps must be finite and >= 0");
+    if (n == 0) return ok();
+    const int e = apc::elem_bytes(dt);
+    if (!x || !out || !aligned_to(x, e) || !aligned_to(out, apc::elem_bytes(out_dt)) || !aligned_to(res, e) ||
+        !aligned_to(weight, e) || !aligned_to(sum, e) || !aligned_to(out_scale, 4))
+        return fail(APC_E_ARG, "apc_norm_rows: x and out are required, every pointer aligned to its elements");
+    if (sum && !res) return fail(APC_E_ARG, "apc_norm_rows: sum is the sum with a residual: res is NULL");
+    if (ld_x < d || ld_out < d || (res && ld_res < d) || (sum && ld_sum < d))
+        return fail(APC_E_ARG, "apc_norm_rows: a row stride is smaller than d = %d", d);
+    if ((out_dt == APC_E4M3) != (out_scale != nullptr))
+        return fail(APC_E_ARG, "apc_norm_rows: out_scale is required for e4m3 and only for e4m3");
+    const apc::NormArgs a{x, res, weight, sum, out, out_scale, n, ld_x, ld_res, ld_sum, ld_out, d, eps};
+    hipError_t err = apc::launch_norm_rows(dt, out_dt, a, static_cast<hipStream_t>(stream));
+    if (err != hipSuccess) return hip_fail(err, "apc_norm_rows launch");
+    return ok();
+}
+
+apc_status apc_kv_write(const apc_kv* c, apc_dtype dt, int64_t t, const void* k, int64_t k_tok, int64_t k_head,
+                        const void* v, int64_t v_tok, int64_t v_head, const int32_t* slots, void* stream)
+{
+    return kv_rows("apc_kv_write", true, c, dt, t, k, k_tok, k_head, v, v_tok, v_head, slots, stream);
+}
+
+apc_status apc_kv_read(const apc_kv* c, apc_dtype dt, int64_t t, const int32_t* slots, void* k, int64_t k_tok,
+                       int64_t k_head, void* v, int64_t v_tok, int64_t v_head, void* stream)
+{
+    return kv_rows("apc_kv_read", false, c, dt, t, k, k_tok, k_head, v, v_tok, v_head, slots, stream);
+}
+
+static apc_status check_attend(const char* who, const apc_kv* c, int32_t b, int32_t q_heads, int32_t max_pages)
+{
+    if (apc_status st = check_kv(who, c)) return st;
+    if (b < 0 || q_heads < 1 || q_heads % c->heads != 0 || (int64_t)b * q_heads > INT32_MAX / 4)
+        return fail(APC_E_ARG, "%s: need b >= 0, q_heads a multiple of the cache's %d heads and b * q_heads < 2^29 "
+                    "(b=%d q_heads=%d)", who, c->heads, b, q_heads);
+    if (max_pages < 0 || max_pages > INT32_MAX / c->page)
+        return fail(APC_E_ARG, "%s: need 0 <= max_pages * page < 2^31 (max_pages=%d)", who, max_pages);
+    return APC_OK;
+}
+
+apc_status apc_attend_workspace(const apc_kv* c, int32_t b, int32_t q_heads, int32_t max_pages, size_t* bytes)
+{
+    if (!bytes) return fail(APC_E_ARG, "apc_attend_workspace: bytes is NULL");
+    if (apc_status st = check_attend("apc_attend_workspace", c, b, q_heads, max_pages)) return st;
+    *bytes = apc::attend_workspace(*c, b, q_heads, max_pages);
+    return ok();
+}
+
+apc_status apc_attend(const apc_kv* c, apc_dtype dt, const void* q, int64_t q_row, int64_t q_head, int32_t b,
+                      int32_t q_heads, const int32_t* pages, int32_t max_pages, int64_t ld_pages,
+                      const int32_t* lengths, int32_t window, float scale, void* out, int64_t out_row,
+                      int64_t out_head, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    if (apc_status st = check_attend("apc_attend", c, b, q_heads, max_pages)) return st;
+    if ((dt != APC_F16 && dt != APC_BF16) || (c->dt != APC_E4M3 && dt != c->dt))
+        return fail(APC_E_DTYPE, "apc_attend: queries are of the cache's type, or f16 or bf16 over e4m3 (got %d)",
+                    (int)dt);
+    if (window < 0) return fail(APC_E_ARG, "apc_attend: window < 0");
+    if (!std::isfinite(scale)) return fail(APC_E_ARG, "apc_attend: scale is not finite");
+    if (q_row < 0 || q_head < 0 || out_row < 0 || out_head < 0 || ld_pages < max_pages)
+        return fail(APC_E_ARG, "apc_attend: negative stride, or ld_pages < max_pages");
+    if (b == 0) return ok();
+    if (!q || !out || !lengths || (max_pages > 0 && !pages) || !aligned_to(q, 2) || !aligned_to(out, 2) ||
+        !aligned_to(pages, 4) || !aligned_to(lengths, 4) || !aligned_to(lse, 4))
+        return fail(APC_E_ARG, "apc_attend: q, out, lengths and pages must be device pointers aligned to their elements");
+    const size_t need = apc::attend_workspace(*c, b, q_heads, max_pages);
+    if (need > 0 && (!ws || !aligned16(ws)))
+        return fail(APC_E_ARG, "apc_attend: workspace must be a non-NULL 16-byte aligned device pointer");
+    if (ws_bytes < need)
+        return fail(APC_E_WORKSPACE, "apc_attend: workspace of %zu bytes, %zu needed", ws_bytes, need);
+    const apc::AttendArgs a{q, out, pages, lengths, lse, ws, q_row, q_head, out_row, out_head, ld_pages,
+                            b, q_heads, max_pages, window, scale};
+    hipError_t err = apc::launch_attend(dt, *c, a, static_cast<hipStream_t>(stream));
+    if (err != hipSuccess) return hip_fail(err, "apc_attend launch");
+    return ok();
 }
 
 }  // extern "C"

@@ -41,6 +41,38 @@ hipError_t launch_row_factors(int dt, int64_t n, int32_t d, const void* rows, co
 hipError_t launch_quantize_rows(int dt, int64_t n, int32_t d, const float* x, void* out, float* scale,
                                 hipStream_t s);
 
+// ---- operators of the prompt model ------------------------------------------
+struct NormArgs {
+    const void *x, *res, *weight;
+    void *sum, *out;
+    float* out_scale;
+    int64_t n, ld_x, ld_res, ld_sum, ld_out;   // strides in elements
+    int32_t d;
+    float eps;
+};
+hipError_t launch_norm_rows(int dt, int out_dt, const NormArgs& a, hipStream_t s);
+
+// rows of tokens on the way into the cache (k, v read) or out of it (written)
+struct KvRows {
+    void *k, *v;
+    const int32_t* slots;
+    int64_t t, k_tok, k_head, v_tok, v_head;
+};
+hipError_t launch_kv_rows(bool write, int dt, const apc_kv& c, const KvRows& a, hipStream_t s);
+
+struct AttendArgs {
+    const void* q;
+    void* out;
+    const int32_t *pages, *lengths;
+    float* lse;
+    void* ws;
+    int64_t q_row, q_head, out_row, out_head, ld_pages;
+    int32_t b, q_heads, max_pages, window;
+    float scale;
+};
+size_t attend_workspace(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages);
+hipError_t launch_attend(int dt, const apc_kv& c, const AttendArgs& a, hipStream_t s);
+
 // factor layout of a cache: n rounded up to a multiple of 256 factors, zeros past n
 __host__ __device__ inline int64_t factor_pad(int64_t n) { return (n + 255) / 256 * 256; }
 

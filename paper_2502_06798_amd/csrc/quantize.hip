@@ -7,49 +7,12 @@
 // integer arithmetic from the formats' definitions.  e4m3fn rows get one
 // float32 scale each: s = amax / 448 (amax = the largest |x| of the row; s = 1
 // when it is not > 0, which includes a row holding NaN), and the codes of
-// clamp(x / s, -448, 448).
+// clamp(x / s, -448, 448).  The roundings are in convert.h.
 #include "apc_internal.h"
+#include "convert.h"
 
 namespace apc {
 namespace {
-
-__device__ inline uint32_t enc_f16(float x)
-{
-    const _Float16 h = (_Float16)x;
-    uint16_t b;
-    __builtin_memcpy(&b, &h, 2);
-    if (x != x) b = (uint16_t)(((__float_as_uint(x) >> 16) & 0x8000u) | 0x7e00u);   // quiet NaN, sign kept
-    return b;
-}
-
-__device__ inline uint32_t enc_bf16(float x)
-{
-    const uint32_t u = __float_as_uint(x);
-    if (x != x) return ((u >> 16) | 0x0040u) & 0xffffu;          // quiet NaN, sign and top payload kept
-    return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;                 // nearest-even; a carry may reach +-Inf
-}
-
-// e4m3fn code of y (|y| <= 448 or NaN), rounded to nearest-even
-__device__ inline uint32_t enc_e4m3(float y)
-{
-    const uint32_t u = __float_as_uint(y);
-    const uint32_t sign = (u >> 24) & 0x80u;
-    if (y != y) return sign | 0x7fu;
-    const uint32_t a = u & 0x7fffffffu;
-    uint32_t code;
-    if (a < 0x3c800000u) {
-        // below 2^-6: the subnormal codes m 2^-9 (m = 8 is the smallest
-        // normal); |y| 512 is exact, rint rounds it to nearest-even
-        code = (uint32_t)__builtin_rintf(__uint_as_float(a) * 512.0f);
-    } else {
-        // keep the top 3 of the 23 mantissa bits, nearest-even (a carry moves
-        // into the exponent), and rebias the exponent from 127 to 7
-        const uint32_t q = a >> 20, rem = a & 0xfffffu;
-        const uint32_t up = rem > 0x80000u || (rem == 0x80000u && (q & 1u)) ? 1u : 0u;
-        code = q + up - ((127u - 7u) << 3);
-    }
-    return sign | code;
-}
 
 template <int DT>
 __global__ __launch_bounds__(256) void k_quantize_rows(const float* __restrict__ x, int64_t n, int32_t d,
