@@ -14,6 +14,18 @@ namespace {
 
 constexpr int PER = APC_MAX_HEAD_DIM / 64;
 
+template <int DT> __device__ inline float one(const typename Elem<DT>::T* p)
+{
+    if constexpr (DT == APC_E4M3) return __builtin_amdgcn_cvt_f32_fp8((int)*p, 0);
+    else {
+        Raw<DT, 1> r;
+        float v;
+        r.load(p);
+        r.values(&v);
+        return v;
+    }
+}
+
 template <int DT, int CDT>
 __global__ __launch_bounds__(64) void k_attend_rows(apc_kv c, AttendArgs a)
 {
@@ -25,7 +37,7 @@ __global__ __launch_bounds__(64) void k_attend_rows(apc_kv c, AttendArgs a)
     float qv[PER], o[PER], m = -3.0e38f, l = 0.f;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-        qv[e] = lane + 64 * e < c.d ? load_elem<DT>(q + lane + 64 * e) * a.scale : 0.f;
+        qv[e] = lane + 64 * e < c.d ? one<DT>(q + lane + 64 * e) * a.scale : 0.f;
         o[e] = 0.f;
     }
     const int64_t cap = (int64_t)a.max_pages * c.page;
@@ -39,7 +51,7 @@ __global__ __launch_bounds__(64) void k_attend_rows(apc_kv c, AttendArgs a)
         float s = 0.f;
 #pragma unroll
         for (int e = 0; e < PER; ++e)
-            if (lane + 64 * e < c.d) s += qv[e] * load_elem<CDT>(static_cast<const C*>(c.k) + row * c.d + lane + 64 * e);
+            if (lane + 64 * e < c.d) s += qv[e] * one<CDT>(static_cast<const C*>(c.k) + row * c.d + lane + 64 * e);
         for (int x = 32; x >= 1; x >>= 1) s += __shfl_xor(s, x, 64);
         float vs = 1.f;
         if constexpr (CDT == APC_E4M3) {
@@ -52,12 +64,14 @@ __global__ __launch_bounds__(64) void k_attend_rows(apc_kv c, AttendArgs a)
 #pragma unroll
         for (int e = 0; e < PER; ++e)
             if (lane + 64 * e < c.d)
-                o[e] = o[e] * was + p1 * vs * load_elem<CDT>(static_cast<const C*>(c.v) + row * c.d + lane + 64 * e);
+                o[e] = o[e] * was + p1 * vs * one<CDT>(static_cast<const C*>(c.v) + row * c.d + lane + 64 * e);
     }
     T* out = static_cast<T*>(a.out) + i * a.out_row + qh * a.out_head;
 #pragma unroll
-    for (int e = 0; e < PER; ++e)
-        if (lane + 64 * e < c.d) store_elem<DT>(out + lane + 64 * e, l == 0.f ? 0.f : o[e] / l);
+    for (int e = 0; e < PER; ++e) {
+            const float v = l == 0.f ? 0.f : o[e] / l;
+            if (lane + 64 * e < c.d) store_values<DT, 1>(out + lane + 64 * e, &v);
+        }
     if (a.lse && lane == 0) a.lse[(int64_t)i * a.q_heads + qh] = l == 0.f ? -INFINITY : m + logf(l);
 }
 

@@ -44,45 +44,124 @@ __device__ inline uint32_t enc_e4m3(float y)
     return sign | code;
 }
 
-// codes of e4m3fn rows: amax (of |x|; NaN elements reported apart) to the row's scale
-__device__ inline float e4m3_scale(float amax, bool nan)
-{
-    const float s = nan ? 1.0f : amax / 448.0f;
-    return s > 0.f ? s : 1.0f;
-}
-
-__device__ inline float e4m3_clamp(float y)
-{
-    return y == y ? __builtin_fminf(__builtin_fmaxf(y, -448.0f), 448.0f) : y;
-}
-
 template <int DT> struct Elem;
 template <> struct Elem<APC_F32> { using T = float; };
 template <> struct Elem<APC_F16> { using T = uint16_t; };
 template <> struct Elem<APC_BF16> { using T = uint16_t; };
 template <> struct Elem<APC_E4M3> { using T = uint8_t; };
 
-template <int DT> __device__ inline float load_elem(const typename Elem<DT>::T* p)
+using f32x2 = float __attribute__((ext_vector_type(2)));
+using f16x2 = _Float16 __attribute__((ext_vector_type(2)));
+using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
+
+// N elements at p as they lie there; p needs only its element's alignment
+// (global loads of 16 bytes may start anywhere)
+template <int DT, int N> struct Raw {
+    static constexpr int BYTES = N * (int)sizeof(typename Elem<DT>::T);
+    uint32_t w[(BYTES + 3) / 4];
+    __device__ void load(const typename Elem<DT>::T* p) { __builtin_memcpy(w, p, BYTES); }
+    __device__ void values(float* v) const
+    {
+        if constexpr (DT == APC_F32) {
+            __builtin_memcpy(v, w, BYTES);
+        } else if constexpr (DT == APC_E4M3) {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) {
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
+                v[4 * i] = lo.x, v[4 * i + 1] = lo.y, v[4 * i + 2] = hi.x, v[4 * i + 3] = hi.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t u = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
+                if constexpr (DT == APC_BF16) {
+                    v[i] = __uint_as_float(u << 16);
+                } else {
+                    const uint16_t s = (uint16_t)u;
+                    _Float16 h;
+                    __builtin_memcpy(&h, &s, 2);
+                    v[i] = (float)h;
+                }
+            }
+        }
+    }
+};
+
+// N values rounded to nearest-even into the type at p, wherever it starts
+// (f32, f16 and bf16: the hardware's conversions, which equal enc_f16 and
+// enc_bf16 on every float32 but for the payload of a half's NaN)
+template <int DT, int N> __device__ inline void store_values(typename Elem<DT>::T* p, const float* v)
 {
     if constexpr (DT == APC_F32) {
-        return *p;
-    } else if constexpr (DT == APC_F16) {
-        _Float16 h;
-        __builtin_memcpy(&h, p, 2);
-        return (float)h;
-    } else if constexpr (DT == APC_BF16) {
-        return __uint_as_float((uint32_t)*p << 16);
+        __builtin_memcpy(p, v, 4 * N);
     } else {
-        return __builtin_amdgcn_cvt_f32_fp8((int)*p, 0);
+        uint32_t w[(N + 1) / 2];
+#pragma unroll
+        for (int i = 0; i < (N + 1) / 2; ++i) {
+            const f32x2 x = {v[2 * i], 2 * i + 1 < N ? v[2 * i + 1] : 0.f};
+            if constexpr (DT == APC_BF16) {
+                const bf16x2 b = __builtin_convertvector(x, bf16x2);
+                __builtin_memcpy(&w[i], &b, 4);
+            } else {
+                const f16x2 h = __builtin_convertvector(x, f16x2);
+                __builtin_memcpy(&w[i], &h, 4);
+            }
+        }
+        __builtin_memcpy(p, w, 2 * N);
     }
 }
 
-template <int DT> __device__ inline void store_elem(typename Elem<DT>::T* p, float x)
-{
-    if constexpr (DT == APC_F32) *p = x;
-    else if constexpr (DT == APC_F16) *p = (uint16_t)enc_f16(x);
-    else if constexpr (DT == APC_BF16) *p = (uint16_t)enc_bf16(x);
-    else *p = (uint8_t)enc_e4m3(x);
-}
+// |x| as an integer: orders like the magnitudes, NaN above infinity
+__device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// Scale of an e4m3fn row from its largest magnitude, and the codes of x / s.
+// With r = 1 / s, q = x r corrected by the remainder x - s q (exact in a fused
+// multiply-add) is the correctly rounded quotient wherever neither r nor the
+// remainder leaves the normal range: s >= 2^-80 leaves it only for quotients
+// below 2^-20, code 0 either way.  Such a row's quotients are at most 448 and
+// two units in the last place, which the hardware's conversion (nearest-even,
+// equal to enc_e4m3 there) takes to 448.  Other rows (NaN, infinite or tiny)
+// divide and round by the definition.
+struct RowCodes {
+    float s, r;
+    bool plain;
+    __device__ explicit RowCodes(uint32_t top)
+    {
+        s = top > 0x7f800000u ? 1.0f : __uint_as_float(top) / 448.0f;
+        if (!(s > 0.f)) s = 1.0f;
+        r = 1.0f / s;
+        plain = top < 0x7f800000u && s >= 0x1p-80f;
+    }
+    __device__ float quotient(float x) const
+    {
+        const float q = x * r;
+        return __builtin_fmaf(__builtin_fmaf(-s, q, x), r, q);
+    }
+    __device__ uint32_t code(float x) const
+    {
+        const float y = x / s;
+        return enc_e4m3(y == y ? __builtin_fminf(__builtin_fmaxf(y, -448.0f), 448.0f) : y);
+    }
+    template <int N> __device__ void store(uint8_t* p, const float* v) const
+    {
+        if constexpr (N == 1) {
+            *p = (uint8_t)code(*v);
+            return;
+        }
+        uint32_t w[(N + 3) / 4];
+        if (plain) {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) {
+                w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(v[4 * i]), quotient(v[4 * i + 1]), 0, false);
+                w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(v[4 * i + 2]), quotient(v[4 * i + 3]), w[i], true);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i)
+                w[i] = code(v[4 * i]) | code(v[4 * i + 1]) << 8 | code(v[4 * i + 2]) << 16 | code(v[4 * i + 3]) << 24;
+        }
+        __builtin_memcpy(p, w, N);
+    }
+};
 
 }  // namespace apc

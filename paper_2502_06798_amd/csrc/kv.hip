@@ -1,105 +1,137 @@
 // Paged key-value cache: new tokens' keys and values written into their slots,
 // rounded or quantised on the way, and slots read back as rows.
 //
-// One wavefront per (token, head, key or value) row of d elements, a lane
-// keeping every 64th.
+// L lanes share a row (one head of one token's key or value), eight elements
+// each, so a row's largest magnitude is a reduction over L lanes and a wave
+// carries 64 / L rows.  A lane keeps the same head and goes on to U tokens, all
+// of whose loads are in flight before the first is converted.  Bound by memory:
+// the rows in and the stored bytes out, once each.
 #include "apc_internal.h"
 #include "convert.h"
 
 namespace apc {
 namespace {
 
-constexpr int64_t MAX_GRID = 1 << 20;   // more rows: a wavefront takes several
-constexpr int PER = APC_MAX_HEAD_DIM / 64;
+constexpr int64_t MAX_GRID = 1 << 20;   // more rows than that many workgroups hold: a lane goes on to further tokens
 
-struct Row {
-    int64_t tok;
-    int32_t head, which;
-};
-
-__device__ inline Row which_row(int64_t r, int32_t heads)
+// row of a slot's head inside k and v (page is a power of two), or -1
+__device__ inline int64_t slot_row(const apc_kv& c, int32_t slot, int32_t head, int shift, int64_t slots)
 {
-    return {r / (2 * heads), (int32_t)(r % (2 * heads)) / 2, (int32_t)(r & 1)};
+    if (slot < 0 || slot >= slots) return -1;
+    return (((int64_t)(slot >> shift) * c.heads + head) << shift) + (slot & (c.page - 1));
 }
 
-// row number of a slot's head inside k and v, or -1
-__device__ inline int64_t slot_row(const apc_kv& c, int32_t slot, int32_t head)
+template <bool WRITE, int DT, int CDT, int L, int U>
+__global__ __launch_bounds__(256) void k_kv_rows(apc_kv c, KvRows a, int shift)
 {
-    if (slot < 0 || slot >= c.n_pages * c.page) return -1;
-    return ((int64_t)(slot / c.page) * c.heads + head) * c.page + slot % c.page;
-}
-
-template <int DT, int CDT>
-__global__ __launch_bounds__(256) void k_kv_write(apc_kv c, KvRows a)
-{
-    using T = typename Elem<DT>::T;
-    using C = typename Elem<CDT>::T;
-    const int lane = threadIdx.x & 63;
-    for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.t * 2 * c.heads; r += (int64_t)gridDim.x * 4) {
-    const Row w = which_row(r, c.heads);
-    const int64_t row = slot_row(c, a.slots[w.tok], w.head);
-    if (row < 0) continue;
-    const T* x = static_cast<const T*>(w.which ? a.v : a.k) +
-                 (w.which ? w.tok * a.v_tok + w.head * a.v_head : w.tok * a.k_tok + w.head * a.k_head);
-    C* out = static_cast<C*>(w.which ? c.v : c.k) + row * c.d;
-    float e[PER], amax = 0.f;
-    bool nan = false;
+    using E = typename Elem<DT>::T;
+    using S = typename Elem<CDT>::T;
+    const int at = threadIdx.x % L * 8;
+    const bool mine = at < c.d;                 // d is a multiple of 16
+    const int64_t slots = c.n_pages << shift;
+    const int32_t rows = 2 * c.heads;           // of a token: every head's key, then every head's value
+    const int64_t unit0 = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L, units = (a.t + U - 1) / U * rows;
+    for (int64_t unit = unit0; unit < units; unit += (int64_t)gridDim.x * (256 / L)) {
+        // t * heads < 2^31, so there are fewer than 2^32 units
+        const uint32_t token = (uint32_t)unit / (uint32_t)rows;
+        const int64_t tok0 = (int64_t)token * U;
+        const int32_t which = (int32_t)((uint32_t)unit - token * (uint32_t)rows), head = which < c.heads ? which : which - c.heads;
+        const bool value = which >= c.heads;
+        E* outer = static_cast<E*>(value ? a.v : a.k) + head * (value ? a.v_head : a.k_head) + at;
+        const int64_t step = value ? a.v_tok : a.k_tok;
+        S* pool = static_cast<S*>(value ? c.v : c.k) + at;
+        float* scale = value ? c.v_scale : c.k_scale;
+        int32_t slot[U];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        e[i] = lane + 64 * i < c.d ? load_elem<DT>(x + lane + 64 * i) : 0.f;
-        nan |= e[i] != e[i];
-        amax = __builtin_fmaxf(amax, __builtin_fabsf(e[i]));
-    }
-    float s = 1.f;
-    if constexpr (CDT == APC_E4M3) {
-        for (int m = 32; m >= 1; m >>= 1) amax = __builtin_fmaxf(amax, __shfl_xor(amax, m, 64));
-        s = e4m3_scale(amax, __any(nan));
-        if (lane == 0) (w.which ? c.v_scale : c.k_scale)[row] = s;
-    }
+        for (int u = 0; u < U; ++u) slot[u] = tok0 + u < a.t ? a.slots[tok0 + u] : -1;
+        if constexpr (WRITE) {
+            Raw<DT, 8> x[U];
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (lane + 64 * i < c.d)
-            store_elem<CDT>(out + lane + 64 * i, CDT == APC_E4M3 ? e4m3_clamp(e[i] / s) : e[i]);
+            for (int u = 0; u < U; ++u)
+                if (mine && tok0 + u < a.t) x[u].load(outer + (tok0 + u) * step);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t row = slot_row(c, slot[u], head, shift, slots);
+                float v[8];
+                x[u].values(v);
+                if constexpr (CDT == APC_E4M3) {
+                    uint32_t top = 0;
+                    if (mine) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) top = magnitude(v[i]) > top ? magnitude(v[i]) : top;
+                    }
+#pragma unroll
+                    for (int m = L / 2; m >= 1; m >>= 1) {
+                        const uint32_t o = __shfl_xor(top, m, 64);
+                        top = o > top ? o : top;
+                    }
+                    const RowCodes codes(top);
+                    if (row >= 0 && mine) {
+                        codes.template store<8>(pool + row * c.d, v);
+                        if (at == 0) scale[row] = codes.s;
+                    }
+                } else {
+                    if (row >= 0 && mine) store_values<CDT, 8>(pool + row * c.d, v);
+                }
+            }
+        } else {
+            Raw<CDT, 8> x[U];
+            float s[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t row = slot_row(c, slot[u], head, shift, slots);
+                s[u] = 1.f;
+                if (row >= 0) {
+                    if (mine) x[u].load(pool + row * c.d);
+                    if constexpr (CDT == APC_E4M3) s[u] = scale[row];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (!mine || tok0 + u >= a.t) continue;
+                float v[8] = {};
+                if (slot[u] >= 0 && slot[u] < slots) {
+                    x[u].values(v);
+                    if constexpr (CDT == APC_E4M3) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] *= s[u];
+                    }
+                }
+                store_values<DT, 8>(outer + (tok0 + u) * step, v);
+            }
+        }
     }
 }
 
-template <int DT, int CDT>
-__global__ __launch_bounds__(256) void k_kv_read(apc_kv c, KvRows a)
+template <bool WRITE, int DT, int CDT, int L>
+void launch_l(const apc_kv& c, const KvRows& a, hipStream_t s)
 {
-    using T = typename Elem<DT>::T;
-    using C = typename Elem<CDT>::T;
-    const int lane = threadIdx.x & 63;
-    for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.t * 2 * c.heads; r += (int64_t)gridDim.x * 4) {
-    const Row w = which_row(r, c.heads);
-    const int64_t row = slot_row(c, a.slots[w.tok], w.head);
-    T* out = static_cast<T*>(w.which ? a.v : a.k) +
-             (w.which ? w.tok * a.v_tok + w.head * a.v_head : w.tok * a.k_tok + w.head * a.k_head);
-    float s = 1.f;
-    if (CDT == APC_E4M3 && row >= 0) s = (w.which ? c.v_scale : c.k_scale)[row];
-    for (int i = lane; i < c.d; i += 64) {
-        float x = 0.f;
-        if (row >= 0) x = load_elem<CDT>(static_cast<const C*>(w.which ? c.v : c.k) + row * c.d + i) * s;
-        store_elem<DT>(out + i, x);
-    }
-    }
-}
-
-template <int DT, int CDT>
-void launch(bool write, const apc_kv& c, const KvRows& a, hipStream_t s)
-{
-    const int64_t groups = (a.t * 2 * c.heads + 3) / 4;
+    int shift = 0;
+    while ((1 << shift) < c.page) ++shift;
+    const int64_t rows = a.t * 2 * c.heads;
+    // four tokens a lane where the rows fill the chip's 2,048 lanes a CU all the same
+    const int u = rows * L >= 4 * 256 * 2048 ? 4 : 1;
+    const int64_t groups = ((a.t + u - 1) / u * 2 * c.heads + 256 / L - 1) / (256 / L);
     const dim3 grid((unsigned)(groups < MAX_GRID ? groups : MAX_GRID)), block(256);
-    if (write) k_kv_write<DT, CDT><<<grid, block, 0, s>>>(c, a);
-    else k_kv_read<DT, CDT><<<grid, block, 0, s>>>(c, a);
+    if (u == 4) k_kv_rows<WRITE, DT, CDT, L, 4><<<grid, block, 0, s>>>(c, a, shift);
+    else k_kv_rows<WRITE, DT, CDT, L, 1><<<grid, block, 0, s>>>(c, a, shift);
 }
 
-template <int DT>
-hipError_t launch_to(bool write, const apc_kv& c, const KvRows& a, hipStream_t s)
+template <bool WRITE, int DT, int CDT>
+void launch(const apc_kv& c, const KvRows& a, hipStream_t s)
+{
+    if (c.d <= 64) launch_l<WRITE, DT, CDT, 8>(c, a, s);
+    else if (c.d <= 128) launch_l<WRITE, DT, CDT, 16>(c, a, s);
+    else launch_l<WRITE, DT, CDT, 32>(c, a, s);
+}
+
+template <bool WRITE, int DT>
+hipError_t launch_to(const apc_kv& c, const KvRows& a, hipStream_t s)
 {
     switch (c.dt) {
-    case APC_F16: launch<DT, APC_F16>(write, c, a, s); break;
-    case APC_BF16: launch<DT, APC_BF16>(write, c, a, s); break;
-    case APC_E4M3: launch<DT, APC_E4M3>(write, c, a, s); break;
+    case APC_F16: launch<WRITE, DT, APC_F16>(c, a, s); break;
+    case APC_BF16: launch<WRITE, DT, APC_BF16>(c, a, s); break;
+    case APC_E4M3: launch<WRITE, DT, APC_E4M3>(c, a, s); break;
     default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -111,9 +143,9 @@ hipError_t launch_kv_rows(bool write, int dt, const apc_kv& c, const KvRows& a, 
 {
     if (a.t <= 0) return hipSuccess;
     switch (dt) {
-    case APC_F32: return launch_to<APC_F32>(write, c, a, s);
-    case APC_F16: return launch_to<APC_F16>(write, c, a, s);
-    case APC_BF16: return launch_to<APC_BF16>(write, c, a, s);
+    case APC_F32: return write ? launch_to<true, APC_F32>(c, a, s) : launch_to<false, APC_F32>(c, a, s);
+    case APC_F16: return write ? launch_to<true, APC_F16>(c, a, s) : launch_to<false, APC_F16>(c, a, s);
+    case APC_BF16: return write ? launch_to<true, APC_BF16>(c, a, s) : launch_to<false, APC_BF16>(c, a, s);
     default: return hipErrorInvalidValue;
     }
 }

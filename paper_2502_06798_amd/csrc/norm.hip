@@ -1,99 +1,204 @@
 // Root-mean-square norm of rows with the residual's addition before it, to the
 // rows' type or to e4m3 codes with a scale per row.
 //
-// One workgroup of 1024 threads per row; a thread keeps every 1024th element
-// of the row in float32 registers, so the row is read once and the sum of
-// squares, the largest |y| and the outputs all come from registers.
+// T threads share a row and keep it in float32 registers, C chunks of 16 bytes
+// each, so the row and the residual are read once and everything after the
+// reduction comes from registers.  One reduction serves both passes: with
+// g = h w, y = g f has its largest magnitude where g has it (f > 0 is the
+// row's; rounding is monotonic), so the sum of squares and the largest |g| are
+// reduced together.  Bound by memory: each row's bytes once.
+//
+// A row that does not end on a chunk ends with a chunk moved back to the row's
+// end: its first `skip` elements are another thread's too, left out of the sum
+// and stored by both with the same bits.  Every load of a row comes before the
+// reduction and every store after it, so that outputs may be the inputs' rows.
 #include "apc_internal.h"
 #include "convert.h"
 
 namespace apc {
 namespace {
 
-constexpr int64_t MAX_GRID = 1 << 20;   // more rows than workgroups: a workgroup takes several
-constexpr int NT = 1024, PER = APC_MAX_NORM_D / NT;
+constexpr int64_t MAX_GRID = 1 << 20;   // more rows than that many workgroups hold: a workgroup takes several
 
-__device__ inline float block_sum(float v, float* red)
+template <int DT, int ODT, int T, int C>
+__global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
 {
-    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int i = 0; i < NT / 64; ++i) v += red[i];
-    return v;
-}
-
-__device__ inline float block_max(float v, float* red)
-{
-    for (int m = 32; m >= 1; m >>= 1) v = __builtin_fmaxf(v, __shfl_xor(v, m, 64));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int i = 0; i < NT / 64; ++i) v = __builtin_fmaxf(v, red[i]);
-    return v;
-}
-
-template <int DT, int ODT>
-__global__ __launch_bounds__(NT) void k_norm_rows(NormArgs a)
-{
-    using T = typename Elem<DT>::T;
+    using E = typename Elem<DT>::T;
     using O = typename Elem<ODT>::T;
-    __shared__ float red[NT / 64];
-    for (int64_t r = blockIdx.x; r < a.n; r += gridDim.x) {
-        const T* x = static_cast<const T*>(a.x) + r * a.ld_x;
-        const T* res = a.res ? static_cast<const T*>(a.res) + r * a.ld_res : nullptr;
-        const T* w = static_cast<const T*>(a.weight);
-        T* sum = a.sum ? static_cast<T*>(a.sum) + r * a.ld_sum : nullptr;
-        O* out = static_cast<O*>(a.out) + r * a.ld_out;
-        float h[PER], ss = 0.f;
+    constexpr int V = 16 / sizeof(E), ROWS = T > 256 ? 1 : 256 / T, WAVES = T / 64;
+    // up to two chunks a thread, the weight is loaded with the row and kept;
+    // longer rows read it twice from the cache, or they would spill registers
+    constexpr bool KEEP_W = C <= 2;
+    __shared__ float red_s[2][WAVES > 1 ? WAVES : 1];
+    __shared__ uint32_t red_m[2][WAVES > 1 ? WAVES : 1];
+    const int t = threadIdx.x % T;
+    int turn = 0;
+    for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; r < a.n; r += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+        const E* x = static_cast<const E*>(a.x) + r * a.ld_x;
+        const E* res = static_cast<const E*>(a.res) + (a.res ? r * a.ld_res : 0);
+        const E* w = static_cast<const E*>(a.weight);
+        Raw<DT, V> rx[C], rr[C], rw[C];   // (rw: KEEP_W only)
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int c = i * NT + threadIdx.x;
-            h[i] = 0.f;
-            if (c < a.d) {
-                h[i] = load_elem<DT>(x + c);
-                if (res) h[i] += load_elem<DT>(res + c);
-                if (sum) store_elem<DT>(sum + c, h[i]);
-                ss += h[i] * h[i];
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V;
+            if (at < a.d) {
+                rx[c].load(x + from);
+                if (a.res) rr[c].load(res + from);
+                if (KEEP_W && a.weight) rw[c].load(w + from);
             }
         }
-        ss = block_sum(ss, red);
+        float h[C][V], ss = 0.f;
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V, skip = at - from;
+            if (at < a.d) {
+                float e[V];
+                if (!KEEP_W && a.weight) rw[c].load(w + from);
+                rx[c].values(h[c]);
+                if (a.res) {
+                    rr[c].values(e);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) h[c][i] += e[i];
+                }
+                if (a.weight) rw[c].values(e);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    ss = i < skip ? ss : __builtin_fmaf(h[c][i], h[c][i], ss);
+                    const uint32_t m = magnitude(a.weight ? h[c][i] * e[i] : h[c][i]);
+                    top = m > top ? m : top;
+                }
+            }
+        }
+#pragma unroll
+        for (int m = (T < 64 ? T : 64) / 2; m >= 1; m >>= 1) {
+            ss += __shfl_xor(ss, m, 64);
+            const uint32_t o = __shfl_xor(top, m, 64);
+            top = o > top ? o : top;
+        }
+        if constexpr (WAVES > 1) {
+            // two sets of cells in turn: a wave may write the next row's while
+            // another still reads this row's
+            if ((threadIdx.x & 63) == 0) {
+                red_s[turn][threadIdx.x >> 6] = ss;
+                red_m[turn][threadIdx.x >> 6] = top;
+            }
+            __syncthreads();
+            ss = 0.f;
+            top = 0;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                ss += red_s[turn][i];
+                top = red_m[turn][i] > top ? red_m[turn][i] : top;
+            }
+        }
         const float f = 1.0f / __builtin_sqrtf(ss / (float)a.d + a.eps);
-        float amax = 0.f, nan = 0.f;
+        // largest |y|; NaN where a g or the row's factor is NaN (0 * inf too)
+        const uint32_t ytop = top > 0x7f800000u ? top : magnitude(__uint_as_float(top) * f);
+        const RowCodes codes(ODT == APC_E4M3 ? ytop : 0u);
+        E* sum = static_cast<E*>(a.sum) + (a.sum ? r * a.ld_sum : 0);
+        O* out = static_cast<O*>(a.out) + r * a.ld_out;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int c = i * NT + threadIdx.x;
-            if (c < a.d) {
-                h[i] *= f;
-                if (w) h[i] *= load_elem<DT>(w + c);
-                if (h[i] != h[i]) nan = 1.f;
-                amax = __builtin_fmaxf(amax, __builtin_fabsf(h[i]));
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V;
+            if (at < a.d) {
+                if (a.sum) store_values<DT, V>(sum + from, h[c]);
+                float y[V];
+                if (!KEEP_W && a.weight) rw[c].load(w + from);
+                if (a.weight) rw[c].values(y);
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = (a.weight ? h[c][i] * y[i] : h[c][i]) * f;
+                if constexpr (ODT == APC_E4M3) codes.store<V>(out + from, y);
+                else store_values<ODT, V>(out + from, y);
             }
+            if constexpr (C >= 4) __builtin_amdgcn_sched_barrier(0);   // chunk by chunk: interleaved, they spill
         }
-        float s = 1.f;
-        if constexpr (ODT == APC_E4M3) {
-            amax = block_max(amax, red);
-            nan = block_max(nan, red);
-            s = e4m3_scale(amax, nan != 0.f);
-            if (threadIdx.x == 0) a.out_scale[r] = s;
-        }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int c = i * NT + threadIdx.x;
-            if (c < a.d) store_elem<ODT>(out + c, ODT == APC_E4M3 ? e4m3_clamp(h[i] / s) : h[i]);
-        }
+        if (ODT == APC_E4M3 && t == 0) a.out_scale[r] = codes.s;
     }
 }
 
-template <int DT>
-hipError_t launch(int out_dt, const NormArgs& a, hipStream_t s)
+// Rows shorter than a chunk: a thread each.
+template <int DT, int ODT>
+__global__ __launch_bounds__(256) void k_norm_short_rows(NormArgs a)
 {
-    const dim3 grid((unsigned)(a.n < MAX_GRID ? a.n : MAX_GRID)), block(NT);
-    if (out_dt == APC_E4M3) k_norm_rows<DT, APC_E4M3><<<grid, block, 0, s>>>(a);
-    else k_norm_rows<DT, DT><<<grid, block, 0, s>>>(a);
+    using E = typename Elem<DT>::T;
+    using O = typename Elem<ODT>::T;
+    constexpr int V = 16 / sizeof(E);
+    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.n; r += (int64_t)gridDim.x * 256) {
+        float h[V], g[V], ss = 0.f;
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < a.d) {
+                Raw<DT, 1> e;
+                e.load(static_cast<const E*>(a.x) + r * a.ld_x + i);
+                e.values(&h[i]);
+                if (a.res) {
+                    float v;
+                    e.load(static_cast<const E*>(a.res) + r * a.ld_res + i);
+                    e.values(&v);
+                    h[i] += v;
+                }
+                g[i] = h[i];
+                if (a.weight) {
+                    float v;
+                    e.load(static_cast<const E*>(a.weight) + i);
+                    e.values(&v);
+                    g[i] *= v;
+                }
+                ss = __builtin_fmaf(h[i], h[i], ss);
+                const uint32_t m = magnitude(g[i]);
+                top = m > top ? m : top;
+            }
+        const float f = 1.0f / __builtin_sqrtf(ss / (float)a.d + a.eps);
+        const RowCodes codes(top > 0x7f800000u ? top : magnitude(__uint_as_float(top) * f));
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < a.d) {
+                const float y = g[i] * f;
+                if (a.sum) store_values<DT, 1>(static_cast<E*>(a.sum) + r * a.ld_sum + i, &h[i]);
+                if constexpr (ODT == APC_E4M3) codes.store<1>(static_cast<O*>(a.out) + r * a.ld_out + i, &y);
+                else store_values<ODT, 1>(static_cast<O*>(a.out) + r * a.ld_out + i, &y);
+            }
+        if (ODT == APC_E4M3) a.out_scale[r] = codes.s;
+    }
+}
+
+template <int DT, int ODT, int T, int C>
+void launch_t(const NormArgs& a, hipStream_t s)
+{
+    constexpr int rows = T > 256 ? 1 : 256 / T;
+    const int64_t groups = (a.n + rows - 1) / rows;
+    k_norm_rows<DT, ODT, T, C><<<dim3((unsigned)(groups < MAX_GRID ? groups : MAX_GRID)), dim3(T > 256 ? T : 256), 0, s>>>(a);
+}
+
+// Threads per row from the row's chunks alone, so that a row's bits do not
+// depend on the call's other rows.
+template <int DT, int ODT>
+hipError_t launch(const NormArgs& a, hipStream_t s)
+{
+    constexpr int V = 16 / sizeof(typename Elem<DT>::T);
+    const int chunks = (a.d + V - 1) / V;
+    if (a.d < V) {
+        const int64_t groups = (a.n + 255) / 256;
+        k_norm_short_rows<DT, ODT><<<dim3((unsigned)(groups < MAX_GRID ? groups : MAX_GRID)), dim3(256), 0, s>>>(a);
+    } else if (chunks <= 16) launch_t<DT, ODT, 16, 1>(a, s);
+    else if (chunks <= 32) launch_t<DT, ODT, 16, 2>(a, s);
+    else if (chunks <= 64) launch_t<DT, ODT, 64, 1>(a, s);
+    else if (chunks <= 128) launch_t<DT, ODT, 64, 2>(a, s);
+    else if (chunks <= 256) launch_t<DT, ODT, 256, 1>(a, s);
+    else if (chunks <= 512) launch_t<DT, ODT, 256, 2>(a, s);
+    else if (chunks <= 1024) launch_t<DT, ODT, 512, 2>(a, s);
+    else if (chunks <= 2048) launch_t<DT, ODT, 1024, 2>(a, s);
+    else if (DT != APC_F32 || chunks <= 4096) launch_t<DT, ODT, 1024, 4>(a, s);
+    else if constexpr (DT == APC_F32) launch_t<DT, ODT, 1024, 8>(a, s);
     return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_to(int out_dt, const NormArgs& a, hipStream_t s)
+{
+    return out_dt == APC_E4M3 ? launch<DT, APC_E4M3>(a, s) : launch<DT, DT>(a, s);
 }
 
 }  // namespace
@@ -102,9 +207,9 @@ hipError_t launch_norm_rows(int dt, int out_dt, const NormArgs& a, hipStream_t s
 {
     if (a.n <= 0) return hipSuccess;
     switch (dt) {
-    case APC_F32: return launch<APC_F32>(out_dt, a, s);
-    case APC_F16: return launch<APC_F16>(out_dt, a, s);
-    case APC_BF16: return launch<APC_BF16>(out_dt, a, s);
+    case APC_F32: return launch_to<APC_F32>(out_dt, a, s);
+    case APC_F16: return launch_to<APC_F16>(out_dt, a, s);
+    case APC_BF16: return launch_to<APC_BF16>(out_dt, a, s);
     default: return hipErrorInvalidValue;
     }
 }
