@@ -70,6 +70,8 @@ typedef enum {
 #define APC_MAX_NORM_D 32768  /* longest row apc_norm_rows takes */
 #define APC_MAX_HEAD_DIM 256  /* largest head of a key-value cache */
 #define APC_MAX_PAGE 1024     /* most tokens of a key-value page */
+#define APC_MAX_TOKENS (1 << 30)       /* most tokens of one sequence's page table */
+#define APC_MAX_ATTEND_ROWS (1 << 23)  /* most sequences x query heads of one apc_attend */
 
 /* opaque, immutable after build */
 typedef struct apc_cache apc_cache;
@@ -517,8 +519,9 @@ apc_status apc_attend_workspace(const apc_kv* c /* host */, int32_t b, int32_t q
  *             cache is APC_E4M3.
  * q, out      sequence i's head a at i * row + a * head elements (strides
  *             q_row, q_head, out_row, out_head >= 0; d contiguous).
- * q_heads     a multiple of the cache's heads.
- * pages       b x max_pages int32 page numbers at row stride ld_pages.
+ * q_heads     a multiple of the cache's heads; b * q_heads <= APC_MAX_ATTEND_ROWS.
+ * pages       b x max_pages int32 page numbers at row stride ld_pages;
+ *             max_pages * page <= APC_MAX_TOKENS.
  * lengths     b int32.
  * window      >= 0.   scale: finite.
  * lse         b x q_heads float32, or NULL.

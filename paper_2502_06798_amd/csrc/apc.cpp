@@ -725,11 +725,12 @@ apc_status apc_kv_read(const apc_kv* c, apc_dtype dt, int64_t t, const int32_t* 
 static apc_status check_attend(const char* who, const apc_kv* c, int32_t b, int32_t q_heads, int32_t max_pages)
 {
     if (apc_status st = check_kv(who, c)) return st;
-    if (b < 0 || q_heads < 1 || q_heads % c->heads != 0 || (int64_t)b * q_heads > INT32_MAX / 4)
-        return fail(APC_E_ARG, "%s: need b >= 0, q_heads a multiple of the cache's %d heads and b * q_heads < 2^29 "
-                    "(b=%d q_heads=%d)", who, c->heads, b, q_heads);
-    if (max_pages < 0 || max_pages > INT32_MAX / c->page)
-        return fail(APC_E_ARG, "%s: need 0 <= max_pages * page < 2^31 (max_pages=%d)", who, max_pages);
+    // a workgroup per query head in the join, and fewer than 2^32 threads in a launch
+    if (b < 0 || q_heads < 1 || q_heads % c->heads != 0 || (int64_t)b * q_heads > APC_MAX_ATTEND_ROWS)
+        return fail(APC_E_ARG, "%s: need b >= 0, q_heads a multiple of the cache's %d heads and b * q_heads <= %d "
+                    "(b=%d q_heads=%d)", who, c->heads, APC_MAX_ATTEND_ROWS, b, q_heads);
+    if (max_pages < 0 || max_pages > APC_MAX_TOKENS / c->page)
+        return fail(APC_E_ARG, "%s: need 0 <= max_pages * page <= %d (max_pages=%d)", who, APC_MAX_TOKENS, max_pages);
     return APC_OK;
 }
 
