@@ -71,6 +71,7 @@ typedef enum {
 #define APC_MAX_HEAD_DIM 256  /* largest head of a key-value cache */
 #define APC_MAX_PAGE 1024     /* most tokens of a key-value page */
 #define APC_MAX_TOKENS (1 << 30)       /* most tokens of one sequence's page table */
+#define APC_MAX_TABLE_TOKENS (1ll << 35)  /* most tokens of all page tables of one apc_attend, 256 added for each */
 #define APC_MAX_ATTEND_ROWS (1 << 23)  /* most sequences x query heads of one apc_attend */
 
 /* opaque, immutable after build */
@@ -521,7 +522,8 @@ apc_status apc_attend_workspace(const apc_kv* c /* host */, int32_t b, int32_t q
  *             q_row, q_head, out_row, out_head >= 0; d contiguous).
  * q_heads     a multiple of the cache's heads; b * q_heads <= APC_MAX_ATTEND_ROWS.
  * pages       b x max_pages int32 page numbers at row stride ld_pages;
- *             max_pages * page <= APC_MAX_TOKENS.
+ *             max_pages * page <= APC_MAX_TOKENS, and over all sequences
+ *             b * (max_pages * page + 256) <= APC_MAX_TABLE_TOKENS.
  * lengths     b int32.
  * window      >= 0.   scale: finite.
  * lse         b x q_heads float32, or NULL.

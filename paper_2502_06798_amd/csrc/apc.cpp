@@ -731,6 +731,9 @@ static apc_status check_attend(const char* who, const apc_kv* c, int32_t b, int3
                     "(b=%d q_heads=%d)", who, c->heads, APC_MAX_ATTEND_ROWS, b, q_heads);
     if (max_pages < 0 || max_pages > APC_MAX_TOKENS / c->page)
         return fail(APC_E_ARG, "%s: need 0 <= max_pages * page <= %d (max_pages=%d)", who, APC_MAX_TOKENS, max_pages);
+    // the kernel counts all sequences' tiles of 32 tokens, and a few more each, in 32 bits
+    if ((int64_t)b * ((int64_t)max_pages * c->page + 256) > APC_MAX_TABLE_TOKENS)
+        return fail(APC_E_ARG, "%s: b page tables of max_pages * page tokens hold more than 2^35", who);
     return APC_OK;
 }
 

@@ -73,21 +73,10 @@ struct AttendArgs {
 struct AttendPlan {
     int32_t shift;       // log2 of the page
     int32_t nq, qtiles;  // query tiles of 16 per wave, workgroups over a group's query heads
-    int32_t splits;      // ranges that a sequence is cut into at most
-    int32_t min_tiles;   // no range is shorter, as long as the sequence is not
-};
-// A sequence's tiles of 32 tokens, cut into `used` ranges of `per` tiles.
-struct Ranges {
-    int tile0, tiles, per, used;
-    __host__ __device__ Ranges(int first, int len, const AttendPlan& p)
-    {
-        tile0 = first / 32;
-        tiles = len > first ? (int)(((int64_t)len + 31) / 32) - tile0 : 0;
-        per = (tiles + p.splits - 1) / p.splits;
-        per = (per + 3) / 4 * 4;                        // four waves take turns
-        per = per < p.min_tiles ? p.min_tiles : per;
-        used = (tiles + per - 1) / per;
-    }
+    int32_t groups;      // workgroups (for each query tile) that share the tiles of all sequences and heads
+    int32_t min_share;   // tiles that a workgroup takes at least, as long as there are as many
+    int32_t snap;        // sequences of up to so many tiles are not cut
+    bool cut;            // some could be longer: stretches of all tiles, joined; else whole units
 };
 size_t attend_workspace(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages);
 hipError_t launch_attend(int dt, const apc_kv& c, const AttendArgs& a, hipStream_t s);

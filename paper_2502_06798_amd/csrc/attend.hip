@@ -1,17 +1,21 @@
 // Attention of one new token per sequence over a paged key-value cache.
 //
-// A workgroup of four waves has one sequence, one key-value head, up to NQ x 16
-// of the query heads that share it, and a range of the sequence's 32-token
-// tiles; wave w takes every fourth tile.  Long sequences are cut into several
-// ranges whose partial results k_attend_join joins.
+// A (sequence, key-value head) pair is a unit, its tokens are cut into tiles of
+// 32.  Where units can be long, the tiles of all units stand in one row (each
+// unit with EXTRA more, for what a unit costs besides its tiles) and every
+// workgroup takes an equal stretch of it, so that ragged lengths leave none with
+// more than its share; a unit that several workgroups share leaves partial
+// results, which k_attend_join joins.  Otherwise a workgroup takes a unit at a
+// time.  For each unit it computes up to NQ x 16 of the query heads
+// that share the key-value head, wave w of four every fourth tile.
 //
 // A tile, per wave, in matrix instructions of 16 x 16 x 32:
 //   S^T = K Q^T    keys are the rows, query heads the columns: a lane holds one
 //                  head's scores of 8 of the 32 keys.  The sum over d runs in
 //                  an order that lets a lane load 16 consecutive elements.
 //   P   = exp2(S - m), float32; m is the head's running maximum, raised (and
-//                  the sums scaled) only where a score passes it by 2^8, so
-//                  that a tile needs no exchange between lanes as a rule.
+//                  the sums scaled) only where a score passes it by 8, so that
+//                  a tile needs no exchange between lanes as a rule.
 //   O^T += V^T P^T the lane's 8 weights are the second operand's 8 values as
 //                  they stand, given that the first operand's lanes load the
 //                  values of the same 8 keys; a lane owns DP / 16 consecutive
@@ -23,7 +27,9 @@
 // exactly to 16 bits; their scales join the scores and the weights in float32.
 //
 // Bound by memory: every key and value is read once, into the registers that
-// the matrix instructions take, the next tile's while this one is computed.
+// the matrix instructions take.  A wave's next tile, of the same unit or of the
+// workgroup's next one, is on its way while this one is computed, joined with
+// the other waves' and stored.
 #include "apc_internal.h"
 #include "convert.h"
 
@@ -72,7 +78,83 @@ template <bool BF, bool HIGH> __device__ inline uint32_t from_e4m3(uint32_t w)
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
 }
 
-template <int DT, int CDT, int DP, int NQ>
+// N dwords of keys or values: read once, so marked not to displace what is in
+// the caches (256 sequences over bf16: 199 us, 209 without; 64 long ones: 578, 598)
+template <int N> __device__ inline void stream(uint32_t* to, const uint8_t* from)
+{
+    if constexpr (N == 1) {
+        *to = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(from));
+    } else {
+        using V = uint32_t __attribute__((ext_vector_type(N)));
+        const V x = __builtin_nontemporal_load(reinterpret_cast<const V*>(from));
+        __builtin_memcpy(to, &x, 4 * N);
+    }
+}
+
+// An entry of an input table at an index that all lanes share.  The tables do
+// not change while the kernel runs, which the compiler cannot know; as constant
+// memory they are read with scalar loads, and what follows from them stays in
+// scalar registers.
+__device__ inline int32_t table_entry(const int32_t* table, int64_t i)
+{
+    return ((const __attribute__((address_space(4))) int32_t*)table)[i];
+}
+
+// a value that every lane holds alike, in scalar registers
+__device__ inline int64_t uniform(int64_t x)
+{
+    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) | (int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
+
+// x / y for x, y > 0, in 32 bits where they suffice
+__device__ inline int64_t quotient(int64_t x, int64_t y)
+{
+    return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
+// a sequence's visible tokens [first, len), and their tiles
+struct Span {
+    int first, len, tile0, tiles;
+    __device__ Span(const AttendArgs& a, const AttendPlan& p, int32_t held)
+    {
+        const int32_t cap = a.max_pages << p.shift;
+        len = held < 0 ? 0 : held < cap ? held : cap;
+        first = a.window > 0 && len > a.window ? len - a.window : 0;
+        tile0 = first / TILE;
+        tiles = (len + TILE - 1) / TILE - tile0;
+    }
+};
+
+// what a unit costs, in tiles: a piece of work begins with its queries and ends
+// with the waves' results joined, which takes about as long as four tiles
+constexpr int EXTRA = 4;
+__device__ inline int cost(int tiles) { return tiles > 0 ? tiles + EXTRA : 0; }
+
+// n tiles of a unit, from its tile `off` on; n = 0 with seq < 0: no work
+struct Piece {
+    int seq, head, off, n;
+    Span span;
+    __device__ int begin() const { return span.tile0 + off; }
+    __device__ int end() const { return span.tile0 + off + n; }
+};
+
+// Workspace: the records (int32), then the partial sums (float32, padded d a
+// row), then their maxima and sums of weights.  Two records a workgroup, of its
+// first cut unit and of its last: the unit, and whether its first tile and its
+// last were in the piece.
+constexpr int32_t REC_START = 1, REC_END = 2;
+__host__ __device__ inline int64_t rec_ints(const AttendPlan& p) { return ((int64_t)p.groups * p.qtiles * 2 + 3) / 4 * 4; }
+__device__ inline float* partial_sums(const AttendArgs& a, const AttendPlan& p)
+{
+    return static_cast<float*>(a.ws) + rec_ints(p);
+}
+__device__ inline float* partial_stats(const AttendArgs& a, const AttendPlan& p, int rows, int dp)
+{
+    return partial_sums(a, p) + (int64_t)p.groups * p.qtiles * 2 * rows * dp;
+}
+
+// CUT: stretches of the row of all tiles; else whole units
+template <int DT, int CDT, int DP, int NQ, bool CUT>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv c, AttendArgs a, AttendPlan p)
 {
     using T = typename Elem<DT>::T;
@@ -81,349 +163,546 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
     constexpr int KW = 4 * ES, VW = EPL * ES / 4;               // dwords: 16 elements of a key, EPL of a value
     constexpr int SL = DP < 128 ? DP : 128;                     // elements of a round of the final sums
     __shared__ float part[WAVES][16][SL + 4];
-    __shared__ float ml[WAVES][NQ * 16][2];
+    __shared__ float ml[2][WAVES][NQ * 16][2];
 
     const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // query tiles of one range come to one XCD (workgroups go round over 8): they read the same keys
-    const int id = blockIdx.x, qt = id / 8 % p.qtiles;
-    const int64_t range = (int64_t)(id / 8 / p.qtiles) * 8 + id % 8;
-    if (range >= (int64_t)a.b * c.heads * p.splits) return;
-    const int unit = (int)(range % ((int64_t)a.b * c.heads)), split = (int)(range / ((int64_t)a.b * c.heads));
-    const int seq = unit / c.heads, head = unit % c.heads, group = a.q_heads / c.heads;
+    // query tiles of one stretch come to one XCD (workgroups go round over 8): they read the same keys
+    const int id = blockIdx.x, qt = id / 8 % p.qtiles, wg = id / 8 / p.qtiles * 8 + id % 8;
+    if (wg >= p.groups) return;
+    const int group = a.q_heads / c.heads, rows = group < NQ * 16 ? group : NQ * 16;
+    auto span_of = [&](int seq) { return Span(a, p, table_entry(a.lengths, seq)); };
 
-    const int32_t held = a.lengths[seq], cap = a.max_pages << p.shift;
-    const int len = held < 0 ? 0 : held < cap ? held : cap;
-    const int first = a.window > 0 && len > a.window ? len - a.window : 0;
-    const Ranges r(first, len, p);
-    if (split > 0 && split >= r.used) return;                   // split 0 of an empty sequence writes its zeros
-    const int begin = r.tile0 + split * r.per, last = r.tile0 + r.tiles;
-    const int end = begin + r.per < last ? begin + r.per : last;
+    Piece cur{0, 0, 0, 0, Span(a, p, 0)};                       // what is worked on
+    int64_t unit_end = (int64_t)a.b * c.heads;                  // CUT: the stretch ends at this unit's tile off_end
+    int off_end = 0;
+    int32_t* rec = static_cast<int32_t*>(a.ws) + ((int64_t)wg * p.qtiles + qt) * 2;
+    if constexpr (CUT) {
+        // sequences that hold nothing, shared out among the workgroups: zeros
+        for (int seq = wg; seq < a.b; seq += p.groups) {
+            if (span_of(seq).tiles > 0) continue;
+            const int h0 = qt * NQ * 16, n = group - h0 < NQ * 16 ? group - h0 : NQ * 16;
+            for (int i = threadIdx.x; i < c.heads * n * c.d; i += 64 * WAVES) {
+                const int d = i % c.d, h = i / c.d / n * group + h0 + i / c.d % n;
+                static_cast<T*>(a.out)[seq * a.out_row + h * a.out_head + d] = 0;
+                if (a.lse && d == 0) a.lse[(int64_t)seq * a.q_heads + h] = -INFINITY;
+            }
+        }
+        // The stretch, found by every wave for itself: a lane has four of every
+        // 256 sequences, their costs (of one head) and the sum up to its last.
+        struct Costs { int held[4], cost[4], upto, total; };
+        auto costs_of = [&](int seq0) {
+            Costs k;
+            int sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int seq = seq0 + lane * 4 + i;
+                k.held[i] = seq < a.b ? a.lengths[seq] : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += k.cost[i] = cost(Span(a, p, k.held[i]).tiles);
+            k.upto = sum;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int o = __shfl_up(k.upto, d, 64);
+                if (lane >= d) k.upto += o;
+            }
+            k.total = __builtin_amdgcn_readlane(k.upto, 63);
+            return k;
+        };
+        const Costs all = costs_of(0);                          // of the first 256; the others are read again
+        int64_t total = all.total;
+        for (int seq0 = 256; seq0 < a.b; seq0 += 256) total += costs_of(seq0).total;
+        total *= c.heads;
+        int64_t share = quotient(total + p.groups - 1, p.groups);
+        share = uniform(share < p.min_share ? p.min_share : share);
+        // A cut inside a unit: of a short one moved to its nearer end, of a
+        // longer one to the nearest multiple of four tiles in proportion.
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t want = (wg + i) * share;
+            if (want >= total) break;
+            const int64_t want_seq = uniform(quotient(want, c.heads));      // want < x heads: want_seq < x
+            Costs k = all;
+            int64_t ahead = 0;                                  // costs (of one head) of the sequences ahead
+            int seq = 0;
+            while (want_seq >= ahead + k.total) {
+                ahead += k.total;
+                seq += 256;
+                k = costs_of(seq);
+            }
+            const int l = __builtin_ctzll(__ballot(k.upto > (int)(want_seq - ahead)));
+            int sum = 0, held = 0, costs = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_readlane(k.cost[e], l);
+            ahead += __builtin_amdgcn_readlane(k.upto, l) - sum;
+            seq += l * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                held = __builtin_amdgcn_readlane(k.held[e], l);
+                costs = __builtin_amdgcn_readlane(k.cost[e], l);
+                if (want_seq < ahead + costs) break;
+                ahead += costs;
+                ++seq;
+            }
+            const int64_t inside = want - ahead * c.heads;
+            const int head = __builtin_amdgcn_readfirstlane((int)quotient(inside, costs));
+            const int at = (int)(inside - (int64_t)head * costs), tiles = costs - EXTRA;
+            // in float32: both neighbours do the same operations on the same numbers
+            const int near = (int)((float)at * ((float)tiles / (float)costs) / WAVES + 0.5f) * WAVES;
+            const int off = __builtin_amdgcn_readfirstlane(tiles <= p.snap ? (2 * at < costs ? 0 : tiles) : near < tiles ? near : tiles);
+            if (i == 0) {
+                cur = Piece{seq, head, off, 0, Span(a, p, held)};
+            } else {
+                unit_end = (int64_t)seq * c.heads + head;
+                off_end = off;
+            }
+        }
+        if (wg * share >= total) {
+            if (threadIdx.x < 2) rec[threadIdx.x] = 0;
+            return;
+        }
+    } else {
+        cur.seq = wg / c.heads, cur.head = wg % c.heads;
+        cur.span = span_of(cur.seq);
+        cur.n = cur.span.tiles;
+    }
+    // the piece after the unit's first u.off tiles, or of the next unit that the stretch reaches
+    auto settle = [&](Piece& u) {
+        int64_t unit = (int64_t)u.seq * c.heads + u.head;
+        while (u.off >= u.span.tiles && unit < unit_end) {
+            u.off = 0;
+            if (u.span.tiles == 0 || ++u.head == c.heads) {
+                u.head = 0;
+                if (++u.seq < a.b) u.span = span_of(u.seq);
+            }
+            unit = (int64_t)u.seq * c.heads + u.head;
+        }
+        u.n = unit < unit_end ? u.span.tiles - u.off : unit == unit_end ? off_end - u.off : 0;
+        if (u.n <= 0) u.seq = -1, u.n = 0;
+    };
+    if constexpr (CUT) {
+        settle(cur);
+        if (cur.seq < 0) {                                      // the cuts moved past each other's units
+            if (threadIdx.x < 2) rec[threadIdx.x] = 0;
+            return;
+        }
+    }
+    auto following = [&](const Piece& u) {
+        Piece v = u;
+        if constexpr (CUT) {
+            v.off += u.n;
+            settle(v);
+        } else {
+            const int64_t unit = (int64_t)u.seq * c.heads + u.head + p.groups;
+            if (unit < (int64_t)a.b * c.heads) {
+                v.seq = (int)(unit / c.heads), v.head = (int)(unit % c.heads);
+                v.span = span_of(v.seq);
+                v.n = v.span.tiles;
+            } else {
+                v.seq = -1, v.n = 0;
+            }
+        }
+        return v;
+    };
 
     // queries: column col of tile n is query head (qt NQ + n) 16 + col of the group
     u32x4 q[NQ][DP / 32];
+    auto load_q = [&](const Piece& u) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const int qh = (qt * NQ + n) * 16 + col;
-        const T* row = static_cast<const T*>(a.q) + seq * a.q_row + (int64_t)(head * group + qh) * a.q_head;
+        for (int n = 0; n < NQ; ++n) {
+            const int qh = (qt * NQ + n) * 16 + col;
+            const T* row = static_cast<const T*>(a.q) + u.seq * a.q_row + (int64_t)(u.head * group + qh) * a.q_head;
 #pragma unroll
-        for (int j = 0; j < DP / 32; ++j) {
-            const int d = j / 2 * 64 + g * 16 + j % 2 * 8;
-            q[n][j] = u32x4{0, 0, 0, 0};
-            if (qh < group && d < c.d) __builtin_memcpy(&q[n][j], row + d, 16);
+            for (int j = 0; j < DP / 32; ++j) {
+                const int d = j / 2 * 64 + g * 16 + j % 2 * 8;
+                q[n][j] = u32x4{0, 0, 0, 0};
+                if (qh < group && d < c.d) __builtin_memcpy(&q[n][j], row + d, 16);
+            }
         }
-    }
-
-    f32x4 o[NQ][EPL];
-    float m[NQ], l[NQ];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        m[n] = LOWEST;
-        l[n] = 0.f;
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) o[n][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    };
 
     // a lane's places in a row; past a row's end (d < DP) it reads another
     // lane's elements: they meet zeros of q, or columns that are not stored
-    const int row_bytes = c.d * ES;
+    const int row_bytes = c.d * ES, in_page = c.page - 1;
     int koff[DP / 64];
 #pragma unroll
     for (int j = 0; j < DP / 64; ++j) koff[j] = col * row_bytes + (j * 64 + g * 16 < c.d ? j * 64 + g * 16 : 0) * ES;
     const int voff = 4 * g * row_bytes + (col * EPL < c.d ? col * EPL : 0) * ES;
-    const int32_t* table = a.pages + seq * a.ld_pages;
-    const int last_page = len > 0 ? (len - 1) >> p.shift : 0, in_page = c.page - 1;
 
-    int32_t pg[2];                                              // of the next tile's halves; -1: none
-    uint32_t kr[2][DP / 64][KW], vr[8][VW];
-    f32x4 ks[2], vs[2];
-    auto find = [&](int t) {
+    struct Pages { int32_t id[2]; };                            // of a tile's halves
+    auto find = [&](const Piece& u, int t) {
+        const int32_t* table = a.pages + u.seq * a.ld_pages;
+        const int last = (u.span.len - 1) >> p.shift;
+        Pages pg;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int at = (t * TILE + 16 * h) >> p.shift;
-            pg[h] = table[at < last_page ? at : last_page];
+            pg.id[h] = table_entry(table, at < last ? at : last);
         }
+        return pg;
     };
-    auto row_of = [&](int t, int h, int32_t pgh) {              // first row of a half tile (page 0 where there is none)
-        const uint32_t page = (uint32_t)pgh < (uint64_t)c.n_pages ? (uint32_t)pgh : 0u;
-        return (((int64_t)page * c.heads + head) << p.shift) + ((t * TILE + 16 * h) & in_page);
+    auto there = [&](int32_t page) { return (uint32_t)page < (uint64_t)c.n_pages; };
+    struct Rows { int64_t at[2]; };                             // first rows of a tile's halves (of page 0 where there is none)
+    auto rows_of = [&](int head, int t, const Pages& pg) {
+        Rows r;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            r.at[h] = (((int64_t)(there(pg.id[h]) ? pg.id[h] : 0) * c.heads + head) << p.shift) + ((t * TILE + 16 * h) & in_page);
+        return r;
     };
-    auto load_k = [&](int t, const int64_t* row) {
+    uint32_t kr[2][DP / 64][KW], vr[8][VW];
+    f32x4 ks[2], vs[2];
+    auto load_k = [&](const Rows& r) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint8_t* base = static_cast<const uint8_t*>(c.k) + row[h] * row_bytes;
+            const uint8_t* base = static_cast<const uint8_t*>(c.k) + r.at[h] * row_bytes;
 #pragma unroll
-            for (int j = 0; j < DP / 64; ++j) __builtin_memcpy(kr[h][j], __builtin_assume_aligned(base + koff[j], 16), 16 * ES);
-            if constexpr (E8) ks[h] = *reinterpret_cast<const f32x4*>(c.k_scale + row[h] + 4 * g);
+            for (int j = 0; j < DP / 64; ++j)
+#pragma unroll
+                for (int w = 0; w < KW; w += 4) stream<4>(kr[h][j] + w, base + koff[j] + w * 4);
+            if constexpr (E8) ks[h] = *reinterpret_cast<const f32x4*>(c.k_scale + r.at[h] + 4 * g);
         }
     };
-    auto load_v = [&](int t, const int64_t* row) {
+    auto load_v = [&](const Rows& r) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint8_t* base = static_cast<const uint8_t*>(c.v) + row[h] * row_bytes;
+            const uint8_t* base = static_cast<const uint8_t*>(c.v) + r.at[h] * row_bytes;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                __builtin_memcpy(vr[4 * h + i], __builtin_assume_aligned(base + voff + i * row_bytes, EPL * ES < 16 ? EPL * ES : 16), EPL * ES);
-            if constexpr (E8) vs[h] = *reinterpret_cast<const f32x4*>(c.v_scale + row[h] + 4 * g);
+#pragma unroll
+                for (int w = 0; w < VW; w += 4) stream<(VW < 4 ? VW : 4)>(vr[4 * h + i] + w, base + voff + i * row_bytes + w * 4);
+            if constexpr (E8) vs[h] = *reinterpret_cast<const f32x4*>(c.v_scale + r.at[h] + 4 * g);
         }
     };
 
     const float to_log2 = a.scale * LOG2E;
-    int t = begin + wave;
-    int64_t row[2];
-    int32_t pc[2];                                              // this tile's pages
-    if (t < end) {
-        find(t);
-        pc[0] = pg[0], pc[1] = pg[1];
-        row[0] = row_of(t, 0, pc[0]), row[1] = row_of(t, 1, pc[1]);
-        load_k(t, row);
-        load_v(t, row);
-        if (t + WAVES < end) find(t + WAVES);
+    int parts = 0;                                              // partial results written
+    int turn = 0;
+    int t = cur.begin() + wave;                                 // this wave's tile, loaded or on its way
+    Pages pc{};                                                 // its pages
+    if (t < cur.end()) {
+        pc = find(cur, t);
+        const Rows r = rows_of(cur.head, t, pc);
+        load_k(r);
+        load_v(r);
     }
-    while (t < end) {
-        const int next = t + WAVES;
-        // scores
-        f32x4 s[NQ][2];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                s[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < DP / 32; ++j) {
-                    u32x4 k;
-                    if constexpr (E8) {
-                        const uint32_t lo = kr[h][j / 2][j % 2 * 2], hi = kr[h][j / 2][j % 2 * 2 + 1];
-                        k = u32x4{from_e4m3<QBF, false>(lo), from_e4m3<QBF, true>(lo), from_e4m3<QBF, false>(hi),
-                                  from_e4m3<QBF, true>(hi)};
-                    } else {
-                        __builtin_memcpy(&k, &kr[h][j / 2][j % 2 * 4], 16);
-                    }
-                    s[n][h] = mfma<QBF>(k, q[n][j], s[n][h]);
-                }
-            }
-        f32x4 factor[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            factor[h] = f32x4{to_log2, to_log2, to_log2, to_log2};
-            if constexpr (E8) factor[h] *= ks[h];
+    load_q(cur);
+    while (true) {
+        const int end = cur.end();
+        const Piece nxt = following(cur);
+        const int t_nxt = nxt.begin() + wave;
+        const bool more = nxt.n > 0 && t_nxt < nxt.end();       // this wave has a tile of the next piece
+        Pages pn{}, pg{};                                       // of the next piece's tile, of the next of this piece
+        if (more) pn = find(nxt, t_nxt);
+        if (t + WAVES < end) pg = find(cur, t + WAVES);
+        if (t >= end && more) {
+            const Rows r = rows_of(nxt.head, t_nxt, pn);
+            load_k(r);
+            load_v(r);
         }
-        int64_t row_next[2] = {0, 0};
-        int32_t pn[2] = {-1, -1};
-        if (next < end) {
-            pn[0] = pg[0], pn[1] = pg[1];
-            row_next[0] = row_of(next, 0, pn[0]), row_next[1] = row_of(next, 1, pn[1]);
-            load_k(next, row_next);
-        }
-#pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) s[n][h] *= factor[h];
-
-        // the first and last tiles, and those with pages that are not there: their unseen keys drop out
-        const bool whole = t * TILE >= first && t * TILE + TILE <= len && (uint32_t)pc[0] < (uint64_t)c.n_pages &&
-                           (uint32_t)pc[1] < (uint64_t)c.n_pages;
-        if (!whole) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int tok = t * TILE + 16 * h + 4 * g + i;
-                    const bool seen = tok >= first && tok < len && (uint32_t)pc[h] < (uint64_t)c.n_pages;
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) s[n][h][i] = seen ? s[n][h][i] : -INFINITY;
-                    if constexpr (E8) vs[h][i] = seen ? vs[h][i] : 0.f;
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) vr[4 * h + i][w] = seen ? vr[4 * h + i][w] : 0u;
-                }
-        }
-
-        // the running maximum
-        float top[NQ];
-        bool over = false;
+        f32x4 o[NQ][EPL];
+        float m[NQ], l[NQ];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            top[n] = s[n][0][0];
+            m[n] = LOWEST;
+            l[n] = 0.f;
 #pragma unroll
-            for (int i = 1; i < 8; ++i) top[n] = __builtin_fmaxf(top[n], s[n][i / 4][i % 4]);
-            over |= top[n] > m[n] + SLACK;
-        }
-        if (__any(over)) {
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                float x = __builtin_fmaxf(m[n], top[n]);
-                x = __builtin_fmaxf(x, __shfl_xor(x, 16, 64));
-                x = __builtin_fmaxf(x, __shfl_xor(x, 32, 64));
-                const float f = __builtin_amdgcn_exp2f(m[n] - x);
-                m[n] = x;
-                l[n] *= f;
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) o[n][e] *= f;
-            }
+            for (int e = 0; e < EPL; ++e) o[n][e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        // weights, in two parts
-        u32x4 hi[NQ], lo[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            float w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(s[n][i / 4][i % 4] - m[n]);
-                l[n] += w[i];
-                if constexpr (E8) w[i] *= vs[i / 4][i % 4];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                hi[n][i] = pack<PBF>(w[2 * i], w[2 * i + 1]);
-                const f32x2 r = unpack<PBF>(hi[n][i]);
-                lo[n][i] = pack<PBF>(w[2 * i] - r.x, w[2 * i + 1] - r.y);
-            }
-        }
-
-        // values: element e of every key's row, keys in pairs
-#pragma unroll
-        for (int w = 0; w < VW; ++w) {
-            constexpr int PER = 4 / ES;
-            u32x4 v[PER];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t x = vr[2 * i][w], y = vr[2 * i + 1][w];
-                if constexpr (E8) {
-                    const uint32_t a01 = __builtin_amdgcn_perm(y, x, 0x05010400u), a23 = __builtin_amdgcn_perm(y, x, 0x07030602u);
-                    v[0][i] = from_e4m3<PBF, false>(a01);
-                    v[1][i] = from_e4m3<PBF, true>(a01);
-                    v[2][i] = from_e4m3<PBF, false>(a23);
-                    v[3][i] = from_e4m3<PBF, true>(a23);
-                } else {
-                    v[0][i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                    v[1][i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                }
-            }
+        while (t < end) {
+            const bool inside = t + WAVES < end;
+            // scores
+            f32x4 s[NQ][2];
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int e = 0; e < PER; ++e) {
-                    o[n][w * PER + e] = mfma<PBF>(v[e], hi[n], o[n][w * PER + e]);
-                    o[n][w * PER + e] = mfma<PBF>(v[e], lo[n], o[n][w * PER + e]);
+                for (int h = 0; h < 2; ++h) {
+                    s[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < DP / 32; ++j) {
+                        u32x4 k;
+                        if constexpr (E8) {
+                            const uint32_t lo = kr[h][j / 2][j % 2 * 2], hi = kr[h][j / 2][j % 2 * 2 + 1];
+                            k = u32x4{from_e4m3<QBF, false>(lo), from_e4m3<QBF, true>(lo), from_e4m3<QBF, false>(hi),
+                                      from_e4m3<QBF, true>(hi)};
+                        } else {
+                            __builtin_memcpy(&k, &kr[h][j / 2][j % 2 * 4], 16);
+                        }
+                        s[n][h] = mfma<QBF>(k, q[n][j], s[n][h]);
+                    }
                 }
-        }
-        if (next < end) {
-            load_v(next, row_next);
-            if (next + WAVES < end) find(next + WAVES);
-        }
-        pc[0] = pn[0], pc[1] = pn[1];
-        t = next;
-    }
+            f32x4 factor[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                factor[h] = f32x4{to_log2, to_log2, to_log2, to_log2};
+                if constexpr (E8) factor[h] *= ks[h];
+            }
+            const Rows r = inside ? rows_of(cur.head, t + WAVES, pg) : rows_of(nxt.head, t_nxt, pn);
+            if (inside || more) load_k(r);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[n][h] *= factor[h];
 
-    // the waves' results into one: m and l first, then the outputs' sums, 128 elements of 16 heads a round
+            // the first and last tiles, and those with pages that are not there: their unseen keys drop out
+            const bool whole = t * TILE >= cur.span.first && t * TILE + TILE <= cur.span.len && there(pc.id[0]) && there(pc.id[1]);
+            if (!whole) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        l[n] += __shfl_xor(l[n], 16, 64);
-        l[n] += __shfl_xor(l[n], 32, 64);
-        if (g == 0) {
-            ml[wave][n * 16 + col][0] = m[n];
-            ml[wave][n * 16 + col][1] = l[n];
-        }
-    }
-    const int hrow = threadIdx.x >> 4, dcol = (threadIdx.x & 15) * (SL / 16);
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
+                    for (int i = 0; i < 4; ++i) {
+                        const int tok = t * TILE + 16 * h + 4 * g + i;
+                        const bool seen = tok >= cur.span.first && tok < cur.span.len && there(pc.id[h]);
 #pragma unroll
-        for (int d0 = 0; d0 < DP; d0 += SL) {
-            __syncthreads();
+                        for (int n = 0; n < NQ; ++n) s[n][h][i] = seen ? s[n][h][i] : -INFINITY;
+                        if constexpr (E8) vs[h][i] = seen ? vs[h][i] : 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = (4 * g + i) * EPL - d0;
-                if (d >= 0 && d < SL) {
+                        for (int w = 0; w < VW; ++w) vr[4 * h + i][w] = seen ? vr[4 * h + i][w] : 0u;
+                    }
+            }
+
+            // the running maximum
+            float top[NQ];
+            bool over = false;
 #pragma unroll
-                    for (int e = 0; e < EPL; e += 4)
-                        *reinterpret_cast<f32x4*>(&part[wave][col][d + e]) =
-                            f32x4{o[n][e][i], o[n][e + 1][i], o[n][e + 2][i], o[n][e + 3][i]};
+            for (int n = 0; n < NQ; ++n) {
+                top[n] = s[n][0][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top[n] = __builtin_fmaxf(top[n], s[n][i / 4][i % 4]);
+                over |= top[n] > m[n] + SLACK;
+            }
+            if (__any(over)) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    float y = __builtin_fmaxf(m[n], top[n]);
+                    y = __builtin_fmaxf(y, __shfl_xor(y, 16, 64));
+                    y = __builtin_fmaxf(y, __shfl_xor(y, 32, 64));
+                    const float f = __builtin_amdgcn_exp2f(m[n] - y);
+                    m[n] = y;
+                    l[n] *= f;
+#pragma unroll
+                    for (int e = 0; e < EPL; ++e) o[n][e] *= f;
                 }
             }
-            __syncthreads();
-            const int qh = (qt * NQ + n) * 16 + hrow;
-            if (qh < group && d0 + dcol < c.d) {
-                float top = LOWEST, sum = 0.f, v[SL / 16] = {};
+
+            // weights, in two parts
+            u32x4 hi[NQ], lo[NQ];
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) top = __builtin_fmaxf(top, ml[w][n * 16 + hrow][0]);
+            for (int n = 0; n < NQ; ++n) {
+                float w[8];
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) {
-                    const float f = __builtin_amdgcn_exp2f(ml[w][n * 16 + hrow][0] - top);
-                    sum = __builtin_fmaf(f, ml[w][n * 16 + hrow][1], sum);
-#pragma unroll
-                    for (int i = 0; i < SL / 16; ++i) v[i] = __builtin_fmaf(f, part[w][hrow][dcol + i], v[i]);
+                for (int i = 0; i < 8; ++i) {
+                    w[i] = __builtin_amdgcn_exp2f(s[n][i / 4][i % 4] - m[n]);
+                    l[n] += w[i];
+                    if constexpr (E8) w[i] *= vs[i / 4][i % 4];
                 }
-                if (r.used <= 1) {
-                    const int64_t qrow = (int64_t)head * group + qh;
-                    const float f = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-                    for (int i = 0; i < SL / 16; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
-                    store_values<DT, SL / 16>(static_cast<T*>(a.out) + seq * a.out_row + qrow * a.out_head + d0 + dcol, v);
-                    if (a.lse && d0 + dcol == 0)
-                        a.lse[(int64_t)seq * a.q_heads + qrow] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
-                } else {
-                    const int64_t slot = ((int64_t)unit * p.splits + split) * group + qh;
-                    float* po = static_cast<float*>(a.ws) + slot * DP + d0 + dcol;
+                for (int i = 0; i < 4; ++i) {
+                    hi[n][i] = pack<PBF>(w[2 * i], w[2 * i + 1]);
+                    const f32x2 y = unpack<PBF>(hi[n][i]);
+                    lo[n][i] = pack<PBF>(w[2 * i] - y.x, w[2 * i + 1] - y.y);
+                }
+            }
+
+            // values: element e of every key's row, keys in pairs
 #pragma unroll
-                    for (int i = 0; i < SL / 16; i += 4) *reinterpret_cast<f32x4*>(po + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
-                    if (d0 + dcol == 0) {
-                        float* pm = static_cast<float*>(a.ws) + (int64_t)a.b * p.splits * a.q_heads * DP + slot * 2;
-                        pm[0] = top;
-                        pm[1] = sum;
+            for (int w = 0; w < VW; ++w) {
+                constexpr int PER = 4 / ES;
+                u32x4 v[PER];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t y = vr[2 * i][w], z = vr[2 * i + 1][w];
+                    if constexpr (E8) {
+                        const uint32_t a01 = __builtin_amdgcn_perm(z, y, 0x05010400u), a23 = __builtin_amdgcn_perm(z, y, 0x07030602u);
+                        v[0][i] = from_e4m3<PBF, false>(a01);
+                        v[1][i] = from_e4m3<PBF, true>(a01);
+                        v[2][i] = from_e4m3<PBF, false>(a23);
+                        v[3][i] = from_e4m3<PBF, true>(a23);
+                    } else {
+                        v[0][i] = __builtin_amdgcn_perm(z, y, 0x05040100u);
+                        v[1][i] = __builtin_amdgcn_perm(z, y, 0x07060302u);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) {
+                        o[n][w * PER + e] = mfma<PBF>(v[e], hi[n], o[n][w * PER + e]);
+                        o[n][w * PER + e] = mfma<PBF>(v[e], lo[n], o[n][w * PER + e]);
+                    }
+            }
+            if (inside || more) load_v(r);
+            pc = inside ? pg : pn;
+            t += WAVES;
+            if (t + WAVES < end) pg = find(cur, t + WAVES);
+        }
+        if (nxt.seq >= 0) load_q(nxt);
+
+        // the waves' results into one: m and l first, then the outputs' sums, 128 elements of 16 heads a round
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            l[n] += __shfl_xor(l[n], 16, 64);
+            l[n] += __shfl_xor(l[n], 32, 64);
+            if (g == 0) {
+                ml[turn][wave][n * 16 + col][0] = m[n];
+                ml[turn][wave][n * 16 + col][1] = l[n];
+            }
+        }
+        const bool whole_unit = cur.n == cur.span.tiles;
+        const int hrow = threadIdx.x >> 4, dcol = (threadIdx.x & 15) * (SL / 16);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int d0 = 0; d0 < DP; d0 += SL) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = (4 * g + i) * EPL - d0;
+                    if (d >= 0 && d < SL) {
+#pragma unroll
+                        for (int e = 0; e < EPL; e += 4)
+                            *reinterpret_cast<f32x4*>(&part[wave][col][d + e]) =
+                                f32x4{o[n][e][i], o[n][e + 1][i], o[n][e + 2][i], o[n][e + 3][i]};
+                    }
+                }
+                __syncthreads();
+                const int qh = (qt * NQ + n) * 16 + hrow;
+                if (qh < group && d0 + dcol < c.d) {
+                    float top = LOWEST, sum = 0.f, v[SL / 16] = {};
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) top = __builtin_fmaxf(top, ml[turn][w][n * 16 + hrow][0]);
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) {
+                        const float f = __builtin_amdgcn_exp2f(ml[turn][w][n * 16 + hrow][0] - top);
+                        sum = __builtin_fmaf(f, ml[turn][w][n * 16 + hrow][1], sum);
+#pragma unroll
+                        for (int i = 0; i < SL / 16; ++i) v[i] = __builtin_fmaf(f, part[w][hrow][dcol + i], v[i]);
+                    }
+                    if (!CUT || whole_unit) {
+                        const int64_t qrow = (int64_t)cur.head * group + qh;
+                        const float f = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+                        for (int i = 0; i < SL / 16; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
+                        store_values<DT, SL / 16>(static_cast<T*>(a.out) + cur.seq * a.out_row + qrow * a.out_head + d0 + dcol, v);
+                        if (a.lse && d0 + dcol == 0)
+                            a.lse[(int64_t)cur.seq * a.q_heads + qrow] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+                    } else {
+                        const int64_t slot = (((int64_t)wg * p.qtiles + qt) * 2 + parts) * rows + n * 16 + hrow;
+                        float* po = partial_sums(a, p) + slot * DP + d0 + dcol;
+#pragma unroll
+                        for (int i = 0; i < SL / 16; i += 4) *reinterpret_cast<f32x4*>(po + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+                        if (d0 + dcol == 0) {
+                            float* pm = partial_stats(a, p, rows, DP) + slot * 2;
+                            pm[0] = top;
+                            pm[1] = sum;
+                        }
                     }
                 }
             }
+        if (CUT && !whole_unit) {
+            if (threadIdx.x == 0)
+                rec[parts] = (cur.off == 0 ? REC_START : 0) | (cur.off + cur.n == cur.span.tiles ? REC_END : 0) |
+                             (cur.seq * c.heads + cur.head) << 2;
+            ++parts;
         }
+        if (nxt.seq < 0) break;
+        // the next piece; its ml is another one, while this one's is still read
+        if (t >= end && !(cur.begin() + wave < end)) pc = pn;   // no tile in this piece: pc is still to be set
+        cur = nxt;
+        t = t_nxt;
+        turn ^= 1;
+    }
+    if (CUT && (int)threadIdx.x >= parts && threadIdx.x < 2) rec[threadIdx.x] = 0;
 }
 
-// Joins a sequence's ranges: one workgroup per query head, its threads over
-// (part of the ranges) x (elements).
-template <int DT, int DP>
-__global__ __launch_bounds__(256) void k_attend_join(apc_kv c, AttendArgs a, AttendPlan p)
+// Joins the cut units: the workgroups that shared one are neighbours, and each
+// one's part is its first but for the one that began the unit.  A workgroup for
+// every unit, or for every stretch where there are fewer (a stretch begins at
+// most one unit that it does not end), and query head, its threads over (some
+// of the parts) x (elements).
+template <int DT, int DP, int JOIN>
+__global__ __launch_bounds__(JOIN) void k_attend_join(apc_kv c, AttendArgs a, AttendPlan p, int rows, bool by_unit)
 {
     using T = typename Elem<DT>::T;
-    constexpr int LANES = DP / 4, PARTS = 256 / LANES;
+    constexpr int LANES = DP / 4, PARTS = JOIN / LANES, AHEAD = 4;
     __shared__ float acc[PARTS][DP];
-    __shared__ float sums[PARTS];
-    const int seq = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads, group = a.q_heads / c.heads;
-    const int head = qh / group;
-    const int32_t held = a.lengths[seq], cap = a.max_pages << p.shift;
-    const int len = held < 0 ? 0 : held < cap ? held : cap;
-    const Ranges r(a.window > 0 && len > a.window ? len - a.window : 0, len, p);
-    if (r.used <= 1) return;                                    // written by its only range
-    const int64_t slot0 = ((int64_t)seq * c.heads + head) * p.splits * group + qh % group;
-    const float* po = static_cast<const float*>(a.ws);
-    const float* pm = po + (int64_t)a.b * p.splits * a.q_heads * DP;
+    __shared__ float sums[PARTS], tops[PARTS];
+    __shared__ int from, to;                                    // record that begins the unit, workgroup that ends it
+    const int of = blockIdx.x / p.qtiles, qt = blockIdx.x % p.qtiles, h = blockIdx.y, group = a.q_heads / c.heads;
+    if (qt * p.nq * 16 + h >= group) return;
+    const int32_t* rec = static_cast<const int32_t*>(a.ws);
+    auto record = [&](int i) { return rec[((int64_t)(i / 2) * p.qtiles + qt) * 2 + i % 2]; };
+    if (threadIdx.x == 0) from = -1, to = -1;
+    __syncthreads();
+    int unit = of;
+    if (by_unit) {
+        for (int i = threadIdx.x; i < 2 * p.groups; i += JOIN) {
+            const int32_t r = record(i);
+            if (r >> 2 == unit && (r & REC_START)) from = i;    // at most one of each
+            if (r >> 2 == unit && (r & REC_END)) to = i / 2;
+        }
+        __syncthreads();
+    } else {
+        const int32_t r0 = record(2 * of), r1 = record(2 * of + 1);
+        const int which = (r0 & 3) == REC_START ? 0 : (r1 & 3) == REC_START ? 1 : -1;
+        if (which < 0) return;
+        unit = (which ? r1 : r0) >> 2;
+        for (int i = of + 1 + threadIdx.x; i < p.groups; i += JOIN) {
+            const int32_t r = record(2 * i);
+            if (r >> 2 == unit && (r & REC_END)) to = i;
+        }
+        if (threadIdx.x == 0) from = 2 * of + which;
+        __syncthreads();
+    }
+    if (from < 0 || to < 0) return;                             // not cut
+    const int wg0 = from / 2, which = from % 2, n = to - wg0 + 1;
+    auto slot = [&](int i) { return (((int64_t)(wg0 + i) * p.qtiles + qt) * 2 + (i == 0 ? which : 0)) * rows + h; };
+    const float* po = partial_sums(a, p);
+    const float* pm = partial_stats(a, p, rows, DP);
     const int d = threadIdx.x % LANES * 4, part = threadIdx.x / LANES;
-    float top = LOWEST;
-    for (int i = threadIdx.x & 63; i < r.used; i += 64) top = __builtin_fmaxf(top, pm[(slot0 + (int64_t)i * group) * 2]);
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, m, 64));
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int i = part; i < r.used; i += PARTS) {
-        const int64_t slot = slot0 + (int64_t)i * group;
-        const float f = __builtin_amdgcn_exp2f(pm[slot * 2] - top);
-        sum = __builtin_fmaf(f, pm[slot * 2 + 1], sum);
-        v += f * *reinterpret_cast<const f32x4*>(po + slot * DP + d);
+    float top = LOWEST, sum = 0.f;
+    for (int i0 = part; i0 < n; i0 += PARTS * AHEAD) {
+        f32x4 x[AHEAD];
+        float m[AHEAD], l[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k * PARTS < n ? i0 + k * PARTS : i0;
+            x[k] = *reinterpret_cast<const f32x4*>(po + slot(i) * DP + d);
+            m[k] = pm[slot(i) * 2];
+            l[k] = pm[slot(i) * 2 + 1];
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (i0 + k * PARTS >= n) break;
+            const float y = __builtin_fmaxf(top, m[k]);
+            const float was = __builtin_amdgcn_exp2f(top - y), is = __builtin_amdgcn_exp2f(m[k] - y);
+            v = v * was + x[k] * is;
+            sum = sum * was + l[k] * is;
+            top = y;
+        }
     }
     *reinterpret_cast<f32x4*>(&acc[part][d]) = v;
-    if (threadIdx.x % LANES == 0) sums[part] = sum;
+    if (threadIdx.x % LANES == 0) sums[part] = sum, tops[part] = top;
     __syncthreads();
     if (part > 0) return;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) top = __builtin_fmaxf(top, tops[i]);
     sum = 0.f;
     v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) {
-        sum += sums[i];
-        v += *reinterpret_cast<const f32x4*>(&acc[i][d]);
+        const float f = __builtin_amdgcn_exp2f(tops[i] - top);
+        sum = __builtin_fmaf(f, sums[i], sum);
+        v += f * *reinterpret_cast<const f32x4*>(&acc[i][d]);
     }
     const float f = sum == 0.f ? 0.f : 1.0f / sum;
     const float out[4] = {sum == 0.f ? 0.f : v.x * f, sum == 0.f ? 0.f : v.y * f, sum == 0.f ? 0.f : v.z * f,
                           sum == 0.f ? 0.f : v.w * f};
-    if (d < c.d) store_values<DT, 4>(static_cast<T*>(a.out) + seq * a.out_row + qh * a.out_head + d, out);
+    const int seq = unit / c.heads, qh = unit % c.heads * group + qt * p.nq * 16 + h;
+    if (d < c.d) store_values<DT, 4>(static_cast<T*>(a.out) + seq * a.out_row + (int64_t)qh * a.out_head + d, out);
     if (a.lse && d == 0) a.lse[(int64_t)seq * a.q_heads + qh] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
@@ -431,11 +710,20 @@ int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // query tiles of a wave: two share a key's registers, but wide heads have no registers for them
 int query_tiles(int d, int group) { return group > 16 && padded(d) <= 128 ? 2 : 1; }
 
-// Ranges per sequence: enough workgroups to fill the chip, none shorter than
-// MIN_TILES where the table could hold the tiles; sequences are cut evenly by
-// their own length in the kernel.
-constexpr int MIN_TILES = 8;
-constexpr int64_t TARGET = 2048;        // workgroups
+constexpr int SNAP = 16;                // units of up to so many tiles are not cut
+constexpr int MIN_SHARE = 8;            // tiles of a stretch, at least
+// Stretches: the workgroups that the chip holds at once.  Two a CU (64 long
+// sequences over e4m3: 530 us; one 624, three 550, four 535); four with rows of
+// 64 bytes, whose tiles are small (64 sequences of 8,192 to 16,384 tokens, 12
+// heads of 64, e4m3: 220 us, 230 with two); one with wide heads, which leave
+// registers for one (32 sequences of 4,096 to 8,192, 4 heads of 256, bf16: 148
+// us, 160 with two).
+int stretches(const apc_kv& c, int qtiles)
+{
+    const int groups = padded(c.d) > 128 ? 256 : c.d * elem_bytes(c.dt) <= 64 ? 1024 : 512;
+    return groups / qtiles > 0 ? groups / qtiles : 1;
+}
+constexpr int64_t UNCUT_GROUPS = 1 << 16;
 AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages)
 {
     AttendPlan p{};
@@ -443,26 +731,48 @@ AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages)
     while ((1 << p.shift) < c.page) ++p.shift;
     p.nq = query_tiles(c.d, group);
     p.qtiles = (group + 16 * p.nq - 1) / (16 * p.nq);
-    const int64_t units = (int64_t)b * c.heads * p.qtiles, tiles = (((int64_t)max_pages << p.shift) + TILE - 1) / TILE + 1;
-    const int64_t most = (tiles + MIN_TILES - 1) / MIN_TILES, want = units > 0 ? (TARGET + units - 1) / units : 1;
-    p.splits = (int32_t)(want < most ? want : most);
-    p.min_tiles = MIN_TILES;
+    p.snap = SNAP;
+    p.min_share = MIN_SHARE;
+    const int64_t units = (int64_t)b * c.heads, tiles = (((int64_t)max_pages << p.shift) + TILE - 1) / TILE;
+    p.cut = tiles > SNAP;
+    int64_t groups = units < UNCUT_GROUPS ? units : UNCUT_GROUPS;
+    if (p.cut) {
+        const int64_t shares = (units * (tiles + EXTRA) + MIN_SHARE - 1) / MIN_SHARE, most = stretches(c, p.qtiles);
+        groups = shares < most ? shares : most;
+    }
+    p.groups = (int32_t)groups;
     return p;
+}
+
+template <int DT, int CDT, int DP, int NQ>
+hipError_t launch_q(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hipStream_t s)
+{
+    const dim3 grid((unsigned)((p.groups + 7) / 8 * 8 * p.qtiles)), block(64 * WAVES);
+    if (!p.cut) {
+        k_attend<DT, CDT, DP, NQ, false><<<grid, block, 0, s>>>(c, a, p);
+        return hipGetLastError();
+    }
+    k_attend<DT, CDT, DP, NQ, true><<<grid, block, 0, s>>>(c, a, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int group = a.q_heads / c.heads, rows = group < NQ * 16 ? group : NQ * 16;
+    const int64_t units = (int64_t)a.b * c.heads;
+    const bool by_unit = units <= p.groups;
+    const dim3 joins((unsigned)((by_unit ? (int)units : p.groups) * p.qtiles), (unsigned)rows);
+    // few units are cut into many parts: more threads to read them (64 parts of
+    // 64 heads: 5.6 us, 7.3 with 256; 2,048 workgroups: 7.5 us, 4.9 with 256)
+    if (joins.x * joins.y <= 512) k_attend_join<DT, DP, 512><<<joins, dim3(512), 0, s>>>(c, a, p, rows, by_unit);
+    else k_attend_join<DT, DP, 256><<<joins, dim3(256), 0, s>>>(c, a, p, rows, by_unit);
+    return hipGetLastError();
 }
 
 template <int DT, int CDT, int DP>
 hipError_t launch_d(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hipStream_t s)
 {
-    const int64_t ranges = ((int64_t)a.b * c.heads * p.splits + 7) / 8 * 8;
-    const dim3 grid((unsigned)(ranges * p.qtiles)), block(64 * WAVES);
     if constexpr (DP <= 128) {
-        if (p.nq == 2) k_attend<DT, CDT, DP, 2><<<grid, block, 0, s>>>(c, a, p);
+        if (p.nq == 2) return launch_q<DT, CDT, DP, 2>(c, a, p, s);
     }
-    if (p.nq == 1) k_attend<DT, CDT, DP, 1><<<grid, block, 0, s>>>(c, a, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.splits <= 1) return e;
-    k_attend_join<DT, DP><<<dim3((unsigned)(a.b * a.q_heads)), dim3(256), 0, s>>>(c, a, p);
-    return hipGetLastError();
+    return launch_q<DT, CDT, DP, 1>(c, a, p, s);
 }
 
 template <int DT, int CDT>
@@ -479,14 +789,10 @@ hipError_t launch(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hip
 
 size_t attend_workspace(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages)
 {
-    // the ranges' sums and statistics; the bound of all smaller batches and tables too
-    const int group = q_heads / c.heads, nq = query_tiles(c.d, group), qtiles = (group + 16 * nq - 1) / (16 * nq);
-    const int64_t rows = (int64_t)b * c.heads, tiles = ((int64_t)max_pages * c.page + TILE - 1) / TILE + 1;
-    const int64_t most = (tiles + MIN_TILES - 1) / MIN_TILES;
-    // splits > 1 only below TARGET units, and then units x splits < TARGET + units
-    const int64_t limit = (TARGET + qtiles - 1) / qtiles, r = rows < limit ? rows : limit;
-    const int64_t ranges = most <= 1 ? 0 : r * most < 2 * limit ? r * most : 2 * limit;
-    return (size_t)ranges * group * (padded(c.d) + 2) * sizeof(float);
+    const AttendPlan p = plan(c, b, q_heads, max_pages);
+    if (!p.cut) return 0;
+    const int group = q_heads / c.heads, rows = group < p.nq * 16 ? group : p.nq * 16;
+    return (size_t)(rec_ints(p) + (int64_t)p.groups * p.qtiles * 2 * rows * (padded(c.d) + 2)) * sizeof(float);
 }
 
 hipError_t launch_attend(int dt, const apc_kv& c, const AttendArgs& args, hipStream_t s)
