@@ -133,8 +133,14 @@ def _ptr(t: Optional[torch.Tensor]):
     return ctypes.c_void_p(t.data_ptr())
 
 
+# The current stream's handle without the Stream object that torch.cuda.current_stream() makes (2.7 us a call, 0.2 so).
+_raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
+        if _raw_stream is not None and _device is not None:
+            return ctypes.c_void_p(_raw_stream(_device()))
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
@@ -371,18 +377,23 @@ def apc_merge_shards(scores: torch.Tensor, idx: torch.Tensor, g: int, b: int, k_
 
 # ---- operators of the prompt model ----
 
-def _rows(t: torch.Tensor, what: str):
-    """Address of a device tensor whose last axis is contiguous."""
-    if not t.is_cuda:
-        raise ValueError(f"{what}: expected a device tensor")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{what}: the last axis must be contiguous")
-    return t.data_ptr()
-
-
-def _like(t: torch.Tensor, what: str, shape, dtype):
+def _view(t: torch.Tensor, what: str, shape, dtype):
+    """(address, strides) of a device tensor of that shape and type whose last axis is contiguous."""
     if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor")
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{what}: the last axis must be contiguous")
+    return t.data_ptr(), strides
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    dt = DTYPE_OF.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{what}: {t.dtype} is none of the library's types")
+    return dt
 
 
 def apc_norm_rows(x: torch.Tensor, out: torch.Tensor, weight: Optional[torch.Tensor] = None,
@@ -390,27 +401,29 @@ def apc_norm_rows(x: torch.Tensor, out: torch.Tensor, weight: Optional[torch.Ten
                   out_scale: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None):
     """Root-mean-square norm of the rows of x (+ res): n x d tensors whose rows may be strided.  out is of x's type
     or float8_e4m3fn (then out_scale holds a float32 scale per row); sum_out, if given, gets x + res."""
-    if x.dim() != 2 or x.dtype not in DTYPE_OF or out.dtype not in DTYPE_OF:
-        raise ValueError("x and out must be 2-D float32/float16/bfloat16 tensors (out: float8_e4m3fn too)")
-    n, d = x.shape
-    _like(out, "out", x.shape, out.dtype)
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2:
+        raise ValueError("x must be a 2-D tensor")
+    n, d = shape
+    dt, odt = _dtype(x, "x"), _dtype(out, "out")
+    xp, xs = _view(x, "x", shape, dtype)
+    op, os_ = _view(out, "out", shape, out.dtype)
+    wp = rp = sp = cp = None
+    rl = sl = d
     if weight is not None:
-        _like(weight, "weight", (d,), x.dtype)
-    for t, what in ((res, "res"), (sum_out, "sum_out")):
-        if t is not None:
-            _like(t, what, x.shape, x.dtype)
+        wp, _ = _view(weight, "weight", (d,), dtype)
+    if res is not None:
+        rp, st = _view(res, "res", shape, dtype)
+        rl = st[0] if n > 1 else d              # of one row, torch's row stride may be anything
+    if sum_out is not None:
+        sp, st = _view(sum_out, "sum_out", shape, dtype)
+        sl = st[0] if n > 1 else d
     if out_scale is not None:
-        _like(out_scale, "out_scale", (n,), torch.float32)
-    _check(load().apc_norm_rows(
-        DTYPE_OF[x.dtype], DTYPE_OF[out.dtype], n, d, _rows(x, "x"), _ld(x),
-        None if res is None else _rows(res, "res"), 0 if res is None else _ld(res), _ptr(weight), eps,
-        None if sum_out is None else _rows(sum_out, "sum_out"), 0 if sum_out is None else _ld(sum_out),
-        _rows(out, "out"), _ld(out), _ptr(out_scale), _stream(stream)))
-
-
-def _ld(t: torch.Tensor) -> int:
-    """Row stride of a 2-D tensor (of one row: its width, whatever stride torch reports)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+        cp, _ = _view(out_scale, "out_scale", (n,), torch.float32)
+    rc = load().apc_norm_rows(dt, odt, n, d, xp, xs[0] if n > 1 else d, rp, rl, wp, eps, sp, sl, op,
+                              os_[0] if n > 1 else d, cp, _stream(stream))
+    if rc:
+        _check(rc)
 
 
 class KvCache:
@@ -420,42 +433,44 @@ class KvCache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
-        if k.dim() != 4 or k.dtype not in DTYPE_OF:
-            raise ValueError("k must be an n_pages x heads x page x d float16/bfloat16/float8_e4m3fn tensor")
-        _like(v, "v", k.shape, k.dtype)
-        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            if t is not None:
-                _like(t, what, k.shape[:3], torch.float32)
+        if k.dim() != 4:
+            raise ValueError("k must be an n_pages x heads x page x d tensor")
+        for t, what, shape, dtype in ((v, "v", k.shape, k.dtype), (k_scale, "k_scale", k.shape[:3], torch.float32),
+                                      (v_scale, "v_scale", k.shape[:3], torch.float32)):
+            if t is not None and (t.shape != shape or t.dtype != dtype):
+                raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.heads, self.page, self.d = k.shape
-        self.struct = _KvStruct(DTYPE_OF[k.dtype], self.heads, self.d, self.page, self.n_pages, _ptr(k), _ptr(v),
+        self.struct = _KvStruct(_dtype(k, "k"), self.heads, self.d, self.page, self.n_pages, _ptr(k), _ptr(v),
                                 _ptr(k_scale), _ptr(v_scale))
         self.ref = ctypes.byref(self.struct)
 
 
 def _kv_rows(c: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
-    t = slots.shape[0]
-    if slots.dim() != 1 or slots.dtype != torch.int32:
+    if slots.dim() != 1:
         raise ValueError("slots must be a 1-D int32 tensor")
-    if k.dtype not in DTYPE_OF:
-        raise ValueError("k and v must be float32/float16/bfloat16 tensors")
-    _like(k, "k", (t, c.heads, c.d), k.dtype)
-    _like(v, "v", (t, c.heads, c.d), k.dtype)
-    return DTYPE_OF[k.dtype], t
+    t = slots.shape[0]
+    shape, dtype = (t, c.heads, c.d), k.dtype
+    kp, ks = _view(k, "k", shape, dtype)
+    vp, vs = _view(v, "v", shape, dtype)
+    sp, ss = _view(slots, "slots", (t,), torch.int32)
+    return _dtype(k, "k"), t, kp, ks[0], ks[1], vp, vs[0], vs[1], sp
 
 
 def apc_kv_write(c: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
     """Keys and values (t x heads x d, tokens and heads strided as they come) into the cache's slots."""
-    dt, t = _kv_rows(c, k, v, slots)
-    _check(load().apc_kv_write(c.ref, dt, t, _rows(k, "k"), k.stride(0), k.stride(1), _rows(v, "v"), v.stride(0),
-                               v.stride(1), _ptr(slots), _stream(stream)))
+    dt, t, kp, kt, kh, vp, vt, vh, sp = _kv_rows(c, k, v, slots)
+    rc = load().apc_kv_write(c.ref, dt, t, kp, kt, kh, vp, vt, vh, sp, _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def apc_kv_read(c: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None):
     """The slots' keys and values into k and v (t x heads x d)."""
-    dt, t = _kv_rows(c, k, v, slots)
-    _check(load().apc_kv_read(c.ref, dt, t, _ptr(slots), _rows(k, "k"), k.stride(0), k.stride(1), _rows(v, "v"),
-                              v.stride(0), v.stride(1), _stream(stream)))
+    dt, t, kp, kt, kh, vp, vt, vh, sp = _kv_rows(c, k, v, slots)
+    rc = load().apc_kv_read(c.ref, dt, t, sp, kp, kt, kh, vp, vt, vh, _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def apc_attend_workspace(c: KvCache, b: int, q_heads: int, max_pages: int) -> int:
@@ -474,16 +489,24 @@ def apc_attend(c: KvCache, q: torch.Tensor, pages: torch.Tensor, lengths: torch.
                out: torch.Tensor, ws: torch.Tensor, lse: Optional[torch.Tensor] = None, window: int = 0, stream=None):
     """Attention of one new token per sequence: q and out b x q_heads x d, pages b x max_pages int32 (page numbers of
     each sequence, rows may be strided), lengths b int32, lse b x q_heads float32 or None."""
-    if q.dim() != 3 or q.dtype not in DTYPE_OF or pages.dim() != 2 or pages.dtype != torch.int32:
-        raise ValueError("q must be a b x q_heads x d float16/bfloat16 tensor and pages a b x max_pages int32 tensor")
-    b, q_heads, d = q.shape
-    _like(out, "out", (b, q_heads, c.d), q.dtype)
-    if d != c.d or pages.shape[0] != b:
-        raise ValueError(f"q has {d} elements a head and the cache {c.d}; pages has {pages.shape[0]} rows for {b}")
-    _like(lengths, "lengths", (b,), torch.int32)
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 3 or pages.dim() != 2:
+        raise ValueError("q must be a b x q_heads x d tensor and pages a b x max_pages int32 tensor")
+    b, q_heads, d = shape
+    max_pages = pages.shape[1]
+    if d != c.d:
+        raise ValueError(f"q has {d} elements a head and the cache {c.d}")
+    qp, qs = _view(q, "q", shape, dtype)
+    op, os_ = _view(out, "out", shape, dtype)
+    pp, ps = _view(pages, "pages", (b, max_pages), torch.int32)
+    lp, _ = _view(lengths, "lengths", (b,), torch.int32)
+    ep = None
     if lse is not None:
-        _like(lse, "lse", (b, q_heads), torch.float32)
-    _check(load().apc_attend(
-        c.ref, DTYPE_OF[q.dtype], _rows(q, "q"), q.stride(0), q.stride(1), b, q_heads, _rows(pages, "pages"),
-        pages.shape[1], _ld(pages), _ptr(lengths), window, scale, _rows(out, "out"), out.stride(0), out.stride(1),
-        _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+        if not lse.is_contiguous():
+            raise ValueError("lse: expected a contiguous tensor")
+        ep, _ = _view(lse, "lse", (b, q_heads), torch.float32)
+    rc = load().apc_attend(c.ref, _dtype(q, "q"), qp, qs[0], qs[1], b, q_heads, pp, max_pages,
+                           ps[0] if b > 1 else max_pages, lp, window, scale, op, os_[0], os_[1], ep, _ptr(ws),
+                           ws.numel() * ws.element_size(), _stream(stream))
+    if rc:
+        _check(rc)
