@@ -73,6 +73,7 @@ struct AttendArgs {
 struct AttendPlan {
     int32_t shift;       // log2 of the page
     int32_t nq, qtiles;  // query tiles of 16 per wave, workgroups over a group's query heads
+    int32_t waves;       // of a workgroup, where units are not cut
     int32_t groups;      // workgroups (for each query tile) that share the tiles of all sequences and heads
     int32_t min_share;   // tiles that a workgroup takes at least, as long as there are as many
     int32_t snap;        // sequences of up to so many tiles are not cut

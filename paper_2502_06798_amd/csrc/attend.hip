@@ -7,7 +7,7 @@
 // more than its share; a unit that several workgroups share leaves partial
 // results, which k_attend_join joins.  Otherwise a workgroup takes a unit at a
 // time.  For each unit it computes up to NQ x 16 of the query heads
-// that share the key-value head, wave w of four every fourth tile.
+// that share the key-value head, wave w of WAVES every WAVES-th tile.
 //
 // A tile, per wave, in matrix instructions of 16 x 16 x 32:
 //   S^T = K Q^T    keys are the rows, query heads the columns: a lane holds one
@@ -38,7 +38,7 @@
 namespace apc {
 namespace {
 
-constexpr int WAVES = 4, TILE = 32;
+constexpr int TILE = 32;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LOWEST = -3.0e38f;      // below every score; finite, so that exp2(-inf - m) is 0
 constexpr float SLACK = 8.f;            // weights stay below 2^8
@@ -154,7 +154,7 @@ __device__ inline float* partial_stats(const AttendArgs& a, const AttendPlan& p,
 }
 
 // CUT: stretches of the row of all tiles; else whole units
-template <int DT, int CDT, int DP, int NQ, bool CUT>
+template <int DT, int CDT, int DP, int NQ, int WAVES, bool CUT>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv c, AttendArgs a, AttendPlan p)
 {
     using T = typename Elem<DT>::T;
@@ -551,7 +551,8 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
             }
         }
         const bool whole_unit = cur.n == cur.span.tiles;
-        const int hrow = threadIdx.x >> 4, dcol = (threadIdx.x & 15) * (SL / 16);
+        constexpr int TPH = 4 * WAVES, PER = SL / TPH;          // threads of a head, elements of a thread
+        const int hrow = threadIdx.x / TPH, dcol = threadIdx.x % TPH * PER;
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -570,7 +571,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                 __syncthreads();
                 const int qh = (qt * NQ + n) * 16 + hrow;
                 if (qh < group && d0 + dcol < c.d) {
-                    float top = LOWEST, sum = 0.f, v[SL / 16] = {};
+                    float top = LOWEST, sum = 0.f, v[PER] = {};
 #pragma unroll
                     for (int w = 0; w < WAVES; ++w) top = __builtin_fmaxf(top, ml[turn][w][n * 16 + hrow][0]);
 #pragma unroll
@@ -578,21 +579,21 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                         const float f = __builtin_amdgcn_exp2f(ml[turn][w][n * 16 + hrow][0] - top);
                         sum = __builtin_fmaf(f, ml[turn][w][n * 16 + hrow][1], sum);
 #pragma unroll
-                        for (int i = 0; i < SL / 16; ++i) v[i] = __builtin_fmaf(f, part[w][hrow][dcol + i], v[i]);
+                        for (int i = 0; i < PER; ++i) v[i] = __builtin_fmaf(f, part[w][hrow][dcol + i], v[i]);
                     }
                     if (!CUT || whole_unit) {
                         const int64_t qrow = (int64_t)cur.head * group + qh;
                         const float f = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-                        for (int i = 0; i < SL / 16; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
-                        store_values<DT, SL / 16>(static_cast<T*>(a.out) + cur.seq * a.out_row + qrow * a.out_head + d0 + dcol, v);
+                        for (int i = 0; i < PER; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
+                        store_values<DT, PER>(static_cast<T*>(a.out) + cur.seq * a.out_row + qrow * a.out_head + d0 + dcol, v);
                         if (a.lse && d0 + dcol == 0)
                             a.lse[(int64_t)cur.seq * a.q_heads + qrow] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
                     } else {
                         const int64_t slot = (((int64_t)wg * p.qtiles + qt) * 2 + parts) * rows + n * 16 + hrow;
                         float* po = partial_sums(a, p) + slot * DP + d0 + dcol;
 #pragma unroll
-                        for (int i = 0; i < SL / 16; i += 4) *reinterpret_cast<f32x4*>(po + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+                        for (int i = 0; i < PER; i += 4) *reinterpret_cast<f32x4*>(po + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
                         if (d0 + dcol == 0) {
                             float* pm = partial_stats(a, p, rows, DP) + slot * 2;
                             pm[0] = top;
@@ -710,7 +711,16 @@ int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // query tiles of a wave: two share a key's registers, but wide heads have no registers for them
 int query_tiles(int d, int group) { return group > 16 && padded(d) <= 128 ? 2 : 1; }
 
-constexpr int SNAP = 16;                // units of up to so many tiles are not cut
+constexpr int SNAP = 16;                // in a stretch, units of up to so many tiles are not cut
+// Up to WIDE_UNITS units, a unit has a workgroup of eight waves, if it has one
+// to itself at all.  It has where even the table's longest would be no more
+// than WHOLE_UNIT bytes, which spares a second launch (64 x 8 units of 1,024
+// tokens, e4m3, heads of 128, 279 KB: 26.5 us, 32.1 in stretches; 4 x 8 of
+// 1,024, bf16, 524 KB: 19.9 and 15.9), or WHOLE_UNIT_MANY where there is a unit
+// for every other CU (32 x 8 of 1,024, bf16: 25.1 us, 31.1 in stretches; 16 x
+// 8: 21.1 and 21.3).
+constexpr int64_t WIDE_UNITS = 256;
+constexpr int64_t WHOLE_UNIT = 288 << 10, WHOLE_UNIT_MANY = 560 << 10;
 constexpr int MIN_SHARE = 8;            // tiles of a stretch, at least
 // Stretches: the workgroups that the chip holds at once.  Two a CU (64 long
 // sequences over e4m3: 530 us; one 624, three 550, four 535); four with rows of
@@ -724,7 +734,7 @@ int stretches(const apc_kv& c, int qtiles)
     return groups / qtiles > 0 ? groups / qtiles : 1;
 }
 constexpr int64_t UNCUT_GROUPS = 1 << 16;
-AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages)
+AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages, int32_t window)
 {
     AttendPlan p{};
     const int group = q_heads / c.heads;
@@ -734,10 +744,14 @@ AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages)
     p.snap = SNAP;
     p.min_share = MIN_SHARE;
     const int64_t units = (int64_t)b * c.heads, tiles = (((int64_t)max_pages << p.shift) + TILE - 1) / TILE;
-    p.cut = tiles > SNAP;
+    // a window bounds the tiles that are seen, too
+    const int64_t seen = window > 0 && window / TILE + 2 < tiles ? window / TILE + 2 : tiles;
+    const int64_t unit_bytes = seen * TILE * 2 * c.d * elem_bytes(c.dt);
+    p.waves = padded(c.d) <= 128 && units * p.qtiles <= WIDE_UNITS && seen > 4 ? 8 : 4;
+    p.cut = unit_bytes > (p.waves == 8 && units >= WIDE_UNITS / 2 ? WHOLE_UNIT_MANY : WHOLE_UNIT);
     int64_t groups = units < UNCUT_GROUPS ? units : UNCUT_GROUPS;
     if (p.cut) {
-        const int64_t shares = (units * (tiles + EXTRA) + MIN_SHARE - 1) / MIN_SHARE, most = stretches(c, p.qtiles);
+        const int64_t shares = (units * (seen + EXTRA) + MIN_SHARE - 1) / MIN_SHARE, most = stretches(c, p.qtiles);
         groups = shares < most ? shares : most;
     }
     p.groups = (int32_t)groups;
@@ -747,12 +761,15 @@ AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages)
 template <int DT, int CDT, int DP, int NQ>
 hipError_t launch_q(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hipStream_t s)
 {
-    const dim3 grid((unsigned)((p.groups + 7) / 8 * 8 * p.qtiles)), block(64 * WAVES);
+    const dim3 grid((unsigned)((p.groups + 7) / 8 * 8 * p.qtiles));
     if (!p.cut) {
-        k_attend<DT, CDT, DP, NQ, false><<<grid, block, 0, s>>>(c, a, p);
+        if constexpr (DP <= 128) {
+            if (p.waves == 8) k_attend<DT, CDT, DP, NQ, 8, false><<<grid, dim3(512), 0, s>>>(c, a, p);
+        }
+        if (p.waves == 4) k_attend<DT, CDT, DP, NQ, 4, false><<<grid, dim3(256), 0, s>>>(c, a, p);
         return hipGetLastError();
     }
-    k_attend<DT, CDT, DP, NQ, true><<<grid, block, 0, s>>>(c, a, p);
+    k_attend<DT, CDT, DP, NQ, 4, true><<<grid, dim3(256), 0, s>>>(c, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int group = a.q_heads / c.heads, rows = group < NQ * 16 ? group : NQ * 16;
@@ -789,7 +806,7 @@ hipError_t launch(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hip
 
 size_t attend_workspace(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages)
 {
-    const AttendPlan p = plan(c, b, q_heads, max_pages);
+    const AttendPlan p = plan(c, b, q_heads, max_pages, 0);
     if (!p.cut) return 0;
     const int group = q_heads / c.heads, rows = group < p.nq * 16 ? group : p.nq * 16;
     return (size_t)(rec_ints(p) + (int64_t)p.groups * p.qtiles * 2 * rows * (padded(c.d) + 2)) * sizeof(float);
@@ -800,7 +817,7 @@ hipError_t launch_attend(int dt, const apc_kv& c, const AttendArgs& args, hipStr
     if (args.b <= 0) return hipSuccess;
     AttendArgs a = args;
     if (c.n_pages == 0) a.max_pages = 0;                        // no page to read from
-    const AttendPlan p = plan(c, a.b, a.q_heads, a.max_pages);
+    const AttendPlan p = plan(c, a.b, a.q_heads, a.max_pages, a.window);
     if (c.dt == APC_E4M3) return dt == APC_F16 ? launch<APC_F16, APC_E4M3>(c, a, p, s) : launch<APC_BF16, APC_E4M3>(c, a, p, s);
     return dt == APC_F16 ? launch<APC_F16, APC_F16>(c, a, p, s) : launch<APC_BF16, APC_BF16>(c, a, p, s);
 }

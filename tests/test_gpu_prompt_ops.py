@@ -26,7 +26,7 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 TORCH = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
 ROUND = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
-TINY = {"f32": 0.0, "f16": 2.0 ** -25, "bf16": 0.0}            # half the smallest subnormal
+TINY = {"f32": 2.0 ** -150, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}   # half the smallest subnormal
 
 
 @pytest.fixture(scope="module")
@@ -435,6 +435,45 @@ def test_attend_split_lengths(apc, orc, cache, dtype, b, heads, group, d, page, 
         check_attend(orc, cache, dtype, pool, table, q, n, d ** -0.5, window, out, lse)
         again = run_attend(apc, pool, table, q, n, d ** -0.5, window)
         assert torch.equal(out, again[0]) and torch.equal(lse, again[1])       # no order of arrival in the result
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("heads,group,d,page", [(1, 1, 16, 16), (3, 2, 64, 64), (2, 5, 80, 16), (2, 4, 128, 32),
+                                                (1, 24, 128, 16), (1, 3, 256, 128), (1, 40, 64, 16)])
+def test_attend_short_sequences_in_a_long_table(apc, orc, cache, dtype, heads, group, d, page):
+    """The table could hold 16,384 tokens a sequence, most of its entries stale."""
+    say(f"attend long table {dtype} over {cache} heads={heads} group={group} d={d} page={page}")
+    pool, table, q = make_attend(d + page, len(LENS), heads, group, d, page, -(-513 // page), cache, dtype)
+    wide = torch.full((len(LENS), 16384 // page), 2 ** 30, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    lens = torch.tensor(LENS, dtype=torch.int32, device="cuda")
+    for window in (0, 70):
+        out, lse = run_attend(apc, pool, wide, q, lens, d ** -0.5, window)
+        check_attend(orc, cache, dtype, pool, table, q, lens, d ** -0.5, window, out, lse)
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("b,heads,group,d,cap,most", [(300, 1, 2, 64, 8192, 40), (1000, 2, 1, 16, 16384, 100),
+                                                      (257, 1, 3, 128, 4096, 700), (5000, 1, 1, 16, 64, 64),
+                                                      (2600, 1, 2, 32, 8192, 33)])
+def test_attend_many_sequences(apc, orc, cache, dtype, b, heads, group, d, cap, most):
+    """Batches past 256 sequences, a third of them empty in runs, in short tables and long ones."""
+    say(f"attend many {dtype} over {cache} b={b} heads={heads} group={group} d={d} cap={cap} most={most}")
+    page, g = 16, gen(b)
+    pages = -(-most // page)
+    pool, small, q = make_attend(b, b, heads, group, d, page, pages, cache, dtype)
+    table = torch.full((b, cap // page), -3, dtype=torch.int32, device="cuda")
+    table[:, :pages] = small
+    lens = torch.randint(0, most + 1, (b,), device="cuda", generator=g).to(torch.int32)
+    lens[b // 5:b // 3] = 0
+    lens[-b // 6:] = 0
+    lens[b // 2] = most
+    for window in (0, 20):
+        out, lse = run_attend(apc, pool, table, q, lens, 0.3, window)
+        check_attend(orc, cache, dtype, pool, small, q, lens, 0.3, window, out, lse)
+    lens.zero_()                                                     # nothing anywhere
+    out, lse = run_attend(apc, pool, table, q, lens, 0.3)
+    assert (out == 0).all() and torch.isneginf(lse).all()
 
 
 @pytest.mark.parametrize("cache,dtype", KINDS)
