@@ -49,6 +49,7 @@ struct NormArgs {
     int64_t n, ld_x, ld_res, ld_sum, ld_out;   // strides in elements
     int32_t d;
     float eps;
+    bool past;          // outputs go past the caches
 };
 hipError_t launch_norm_rows(int dt, int out_dt, const NormArgs& a, hipStream_t s);
 

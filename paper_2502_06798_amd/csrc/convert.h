@@ -87,13 +87,33 @@ template <int DT, int N> struct Raw {
     }
 };
 
+// N dwords to p, wherever it starts.  `past`: marked not to stay in the caches,
+// for outputs larger than they are (whole lines only: a part of a line costs
+// its line's read and write)
+template <int N, typename P> __device__ inline void store_dwords(P* p, const uint32_t* w, bool past)
+{
+    if constexpr (N == 2 || N == 4) {
+        typedef uint32_t V __attribute__((ext_vector_type(N), aligned(1)));
+        if (past) {
+            V x;
+            __builtin_memcpy(&x, w, 4 * N);
+            __builtin_nontemporal_store(x, reinterpret_cast<V*>(p));
+            return;
+        }
+    }
+    __builtin_memcpy(p, w, 4 * N);
+}
+
 // N values rounded to nearest-even into the type at p, wherever it starts
 // (f32, f16 and bf16: the hardware's conversions, which equal enc_f16 and
 // enc_bf16 on every float32 but for the payload of a half's NaN)
-template <int DT, int N> __device__ inline void store_values(typename Elem<DT>::T* p, const float* v)
+template <int DT, int N> __device__ inline void store_values(typename Elem<DT>::T* p, const float* v, bool past = false)
 {
     if constexpr (DT == APC_F32) {
-        __builtin_memcpy(p, v, 4 * N);
+        uint32_t w[N];
+        __builtin_memcpy(w, v, 4 * N);
+#pragma unroll
+        for (int i = 0; i < N; i += 4) store_dwords<(N < 4 ? N : 4)>(p + i, w + i, past);
     } else {
         uint32_t w[(N + 1) / 2];
 #pragma unroll
@@ -107,7 +127,12 @@ template <int DT, int N> __device__ inline void store_values(typename Elem<DT>::
                 __builtin_memcpy(&w[i], &h, 4);
             }
         }
-        __builtin_memcpy(p, w, 2 * N);
+        if constexpr (N % 2 == 0) {
+#pragma unroll
+            for (int i = 0; i < N / 2; i += 4) store_dwords<(N / 2 < 4 ? N / 2 : 4)>(p + 2 * i, w + i, past);
+        } else {
+            __builtin_memcpy(p, w, 2 * N);
+        }
     }
 }
 
@@ -142,7 +167,7 @@ struct RowCodes {
         const float y = x / s;
         return enc_e4m3(y == y ? __builtin_fminf(__builtin_fmaxf(y, -448.0f), 448.0f) : y);
     }
-    template <int N> __device__ void store(uint8_t* p, const float* v) const
+    template <int N> __device__ void store(uint8_t* p, const float* v, bool past = false) const
     {
         if constexpr (N == 1) {
             *p = (uint8_t)code(*v);
@@ -160,7 +185,7 @@ struct RowCodes {
             for (int i = 0; i < N / 4; ++i)
                 w[i] = code(v[4 * i]) | code(v[4 * i + 1]) << 8 | code(v[4 * i + 2]) << 16 | code(v[4 * i + 3]) << 24;
         }
-        __builtin_memcpy(p, w, N);
+        store_dwords<N / 4>(p, w, past);
     }
 };
 

@@ -18,6 +18,9 @@
 namespace apc {
 namespace {
 
+// Bytes of output from which it goes past the caches, where nobody would find
+// it again (65,536 x 1,024 bf16: 88 us, 92 without; 100,000 x 768 f16: 51 and 56).
+constexpr int64_t PAST_CACHES = 64 << 20;
 constexpr int64_t MAX_GRID = 1 << 20;   // more rows than that many workgroups hold: a workgroup takes several
 
 template <int DT, int ODT, int T, int C>
@@ -26,18 +29,23 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
     using E = typename Elem<DT>::T;
     using O = typename Elem<ODT>::T;
     constexpr int V = 16 / sizeof(E), ROWS = T > 256 ? 1 : 256 / T, WAVES = T / 64;
-    // up to two chunks a thread, the weight is loaded with the row and kept;
+    // up to three chunks a thread, the weight is loaded with the row and kept;
     // longer rows read it twice from the cache, or they would spill registers
-    constexpr bool KEEP_W = C <= 2;
-    __shared__ float red_s[2][WAVES > 1 ? WAVES : 1];
-    __shared__ uint32_t red_m[2][WAVES > 1 ? WAVES : 1];
-    const int t = threadIdx.x % T;
+    constexpr bool KEEP_W = C <= 3;
+    constexpr int CELLS = WAVES > 1 ? WAVES : 1;
+    __shared__ float red_s[2][ROWS][CELLS];
+    __shared__ uint32_t red_m[2][ROWS][CELLS];
+    const int t = threadIdx.x % T, own = threadIdx.x / T;
+    const E* w = static_cast<const E*>(a.weight);
     int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; r < a.n; r += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+    // every thread of the workgroup goes round as often: threads past the last
+    // row read that row once more and store nothing
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.n; r0 += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+        const bool live = r0 + own < a.n;
+        const int64_t r = live ? r0 + own : a.n - 1;
         const E* x = static_cast<const E*>(a.x) + r * a.ld_x;
         const E* res = static_cast<const E*>(a.res) + (a.res ? r * a.ld_res : 0);
-        const E* w = static_cast<const E*>(a.weight);
-        Raw<DT, V> rx[C], rr[C], rw[C];   // (rw: KEEP_W only)
+        Raw<DT, V> rx[C], rr[C], rw[C];                         // (rw: KEEP_W only)
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V;
@@ -51,16 +59,20 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
         uint32_t top = 0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            float e[V];
+            rx[c].values(h[c]);
+            if (a.res) {
+                rr[c].values(e);
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[c][i] += e[i];
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
             const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V, skip = at - from;
             if (at < a.d) {
                 float e[V];
                 if (!KEEP_W && a.weight) rw[c].load(w + from);
-                rx[c].values(h[c]);
-                if (a.res) {
-                    rr[c].values(e);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) h[c][i] += e[i];
-                }
                 if (a.weight) rw[c].values(e);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
@@ -80,16 +92,16 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
             // two sets of cells in turn: a wave may write the next row's while
             // another still reads this row's
             if ((threadIdx.x & 63) == 0) {
-                red_s[turn][threadIdx.x >> 6] = ss;
-                red_m[turn][threadIdx.x >> 6] = top;
+                red_s[turn][own][t >> 6] = ss;
+                red_m[turn][own][t >> 6] = top;
             }
             __syncthreads();
             ss = 0.f;
             top = 0;
 #pragma unroll
             for (int i = 0; i < WAVES; ++i) {
-                ss += red_s[turn][i];
-                top = red_m[turn][i] > top ? red_m[turn][i] : top;
+                ss += red_s[turn][own][i];
+                top = red_m[turn][own][i] > top ? red_m[turn][own][i] : top;
             }
         }
         const float f = 1.0f / __builtin_sqrtf(ss / (float)a.d + a.eps);
@@ -101,19 +113,19 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V;
-            if (at < a.d) {
-                if (a.sum) store_values<DT, V>(sum + from, h[c]);
+            if (live && at < a.d) {
+                if (a.sum) store_values<DT, V>(sum + from, h[c], a.past);
                 float y[V];
                 if (!KEEP_W && a.weight) rw[c].load(w + from);
                 if (a.weight) rw[c].values(y);
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] = (a.weight ? h[c][i] * y[i] : h[c][i]) * f;
-                if constexpr (ODT == APC_E4M3) codes.store<V>(out + from, y);
-                else store_values<ODT, V>(out + from, y);
+                if constexpr (ODT == APC_E4M3) codes.store<V>(out + from, y, a.past);
+                else store_values<ODT, V>(out + from, y, a.past);
             }
             if constexpr (C >= 4) __builtin_amdgcn_sched_barrier(0);   // chunk by chunk: interleaved, they spill
         }
-        if (ODT == APC_E4M3 && t == 0) a.out_scale[r] = codes.s;
+        if (ODT == APC_E4M3 && live && t == 0) a.out_scale[r] = codes.s;
     }
 }
 
@@ -173,7 +185,10 @@ void launch_t(const NormArgs& a, hipStream_t s)
 }
 
 // Threads per row from the row's chunks alone, so that a row's bits do not
-// depend on the call's other rows.
+// depend on the call's other rows: the fewest that leave two or three chunks to
+// each, and with them several loads in flight and few threads idle (100,000 x
+// 768 f16: 32 threads with three 56 us, 64 with two 79; 65,536 x 4,096 bf16 with
+// residual to e4m3: 256 with two 318 us, 128 with four 400).
 template <int DT, int ODT>
 hipError_t launch(const NormArgs& a, hipStream_t s)
 {
@@ -184,12 +199,19 @@ hipError_t launch(const NormArgs& a, hipStream_t s)
         k_norm_short_rows<DT, ODT><<<dim3((unsigned)(groups < MAX_GRID ? groups : MAX_GRID)), dim3(256), 0, s>>>(a);
     } else if (chunks <= 16) launch_t<DT, ODT, 16, 1>(a, s);
     else if (chunks <= 32) launch_t<DT, ODT, 16, 2>(a, s);
-    else if (chunks <= 64) launch_t<DT, ODT, 64, 1>(a, s);
+    else if (chunks <= 48) launch_t<DT, ODT, 16, 3>(a, s);
+    else if (chunks <= 64) launch_t<DT, ODT, 32, 2>(a, s);
+    else if (chunks <= 96) launch_t<DT, ODT, 32, 3>(a, s);
     else if (chunks <= 128) launch_t<DT, ODT, 64, 2>(a, s);
-    else if (chunks <= 256) launch_t<DT, ODT, 256, 1>(a, s);
+    else if (chunks <= 192) launch_t<DT, ODT, 64, 3>(a, s);
+    else if (chunks <= 256) launch_t<DT, ODT, 128, 2>(a, s);
+    else if (chunks <= 384) launch_t<DT, ODT, 128, 3>(a, s);
     else if (chunks <= 512) launch_t<DT, ODT, 256, 2>(a, s);
+    else if (chunks <= 768) launch_t<DT, ODT, 256, 3>(a, s);
     else if (chunks <= 1024) launch_t<DT, ODT, 512, 2>(a, s);
+    else if (chunks <= 1536) launch_t<DT, ODT, 512, 3>(a, s);
     else if (chunks <= 2048) launch_t<DT, ODT, 1024, 2>(a, s);
+    else if (chunks <= 3072) launch_t<DT, ODT, 1024, 3>(a, s);
     else if (DT != APC_F32 || chunks <= 4096) launch_t<DT, ODT, 1024, 4>(a, s);
     else if constexpr (DT == APC_F32) launch_t<DT, ODT, 1024, 8>(a, s);
     return hipGetLastError();
@@ -203,9 +225,11 @@ hipError_t launch_to(int out_dt, const NormArgs& a, hipStream_t s)
 
 }  // namespace
 
-hipError_t launch_norm_rows(int dt, int out_dt, const NormArgs& a, hipStream_t s)
+hipError_t launch_norm_rows(int dt, int out_dt, const NormArgs& args, hipStream_t s)
 {
-    if (a.n <= 0) return hipSuccess;
+    if (args.n <= 0) return hipSuccess;
+    NormArgs a = args;
+    a.past = a.n * a.d * elem_bytes(out_dt) >= PAST_CACHES;
     switch (dt) {
     case APC_F32: return launch_to<APC_F32>(out_dt, a, s);
     case APC_F16: return launch_to<APC_F16>(out_dt, a, s);
