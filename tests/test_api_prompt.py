@@ -73,7 +73,7 @@ def test_kv_rows_refusals(lib):
 
         assert call(t=0) == 0
         assert call(cache=None) == E_ARG
-        assert call(dt=E4M3) == E_DTYPE and call(dt=-1) == E_DTYPE
+        assert call(dt=E4M3) == E_DTYPE and call(dt=1 << 30) == E_DTYPE
         assert call(t=-1) == E_ARG and call(t=1 << 31) == E_ARG
         assert call(kt=-1) == E_ARG and call(kh=-1) == E_ARG and call(vt=-1) == E_ARG and call(vh=-1) == E_ARG
         assert call(k=None) == E_ARG and call(v=None) == E_ARG and call(s=None) == E_ARG

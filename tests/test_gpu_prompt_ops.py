@@ -476,6 +476,27 @@ def test_attend_many_sequences(apc, orc, cache, dtype, b, heads, group, d, cap, 
     assert (out == 0).all() and torch.isneginf(lse).all()
 
 
+def test_attend_more_units_than_workgroups(apc, orc):
+    """Short sequences in more (sequence, head) pairs than a launch has workgroups for."""
+    b, heads, d, page = 9000, 8, 16, 16
+    pool, table, q = make_attend(61, b, heads, 1, d, page, 1, "f16", "f16")
+    lens = torch.randint(0, 17, (b,), device="cuda", generator=gen(62)).to(torch.int32)
+    out, lse = run_attend(apc, pool, table, q, lens, 0.25)
+    at = torch.cat([torch.arange(0, 30), torch.arange(8150, 8230), torch.arange(b - 30, b)]).cuda()
+    check_attend(orc, "f16", "f16", pool, table[at], q[at], lens[at], 0.25, 0, out[at], lse[at])
+    assert torch.equal(torch.isneginf(lse).all(dim=1), lens == 0) and (out[lens > 0].abs().amax(dim=2) > 0).all()
+
+
+@pytest.mark.parametrize("cap", [64, 16384])
+def test_attend_without_pages(apc, cap):
+    """A pool of no pages: every entry is outside it."""
+    pool = make_pool(0, 2, 16, 64, "bf16")
+    q = torch.randn((3, 4, 64), device="cuda", generator=gen(63)).to(torch.bfloat16)
+    table = torch.zeros((3, cap // 16), dtype=torch.int32, device="cuda")
+    out, lse = run_attend(apc, pool, table, q, torch.tensor([cap, 5, 0], dtype=torch.int32, device="cuda"), 0.1)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+
+
 @pytest.mark.parametrize("cache,dtype", KINDS)
 @pytest.mark.parametrize("scale", [0.0, -0.125, 3.0])
 def test_attend_peaked_flat_and_rising_scores(apc, orc, cache, dtype, scale):
