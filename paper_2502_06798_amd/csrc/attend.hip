@@ -78,15 +78,20 @@ template <bool BF, bool HIGH> __device__ inline uint32_t from_e4m3(uint32_t w)
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
 }
 
-// N dwords of keys or values: read once, so marked not to displace what is in
-// the caches (256 sequences over bf16: 199 us, 209 without; 64 long ones: 578, 598)
-template <int N> __device__ inline void stream(uint32_t* to, const uint8_t* from)
+// N dwords of keys or values.  ONCE: read by one workgroup only, so marked not
+// to displace what is in the caches (256 sequences over bf16: 199 us, 209
+// without; 64 long ones: 578, 598); but where several workgroups have the query
+// heads of one key-value head, the second finds what the first read (64
+// sequences, 128 query heads on one of 128, bf16: 162 us, 234 past the caches).
+template <int N, bool ONCE> __device__ inline void stream(uint32_t* to, const uint8_t* from)
 {
     if constexpr (N == 1) {
-        *to = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(from));
+        const auto* p = reinterpret_cast<const uint32_t*>(from);
+        *to = ONCE ? __builtin_nontemporal_load(p) : *p;
     } else {
         using V = uint32_t __attribute__((ext_vector_type(N)));
-        const V x = __builtin_nontemporal_load(reinterpret_cast<const V*>(from));
+        const auto* p = reinterpret_cast<const V*>(from);
+        const V x = ONCE ? __builtin_nontemporal_load(p) : *p;
         __builtin_memcpy(to, &x, 4 * N);
     }
 }
@@ -153,8 +158,8 @@ __device__ inline float* partial_stats(const AttendArgs& a, const AttendPlan& p,
     return partial_sums(a, p) + (int64_t)p.groups * p.qtiles * 2 * rows * dp;
 }
 
-// CUT: stretches of the row of all tiles; else whole units
-template <int DT, int CDT, int DP, int NQ, int WAVES, bool CUT>
+// CUT: stretches of the row of all tiles; else whole units.  ONCE: one query tile a group
+template <int DT, int CDT, int DP, int NQ, int WAVES, bool CUT, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv c, AttendArgs a, AttendPlan p)
 {
     using T = typename Elem<DT>::T;
@@ -360,7 +365,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
 #pragma unroll
             for (int j = 0; j < DP / 64; ++j)
 #pragma unroll
-                for (int w = 0; w < KW; w += 4) stream<4>(kr[h][j] + w, base + koff[j] + w * 4);
+                for (int w = 0; w < KW; w += 4) stream<4, ONCE>(kr[h][j] + w, base + koff[j] + w * 4);
             if constexpr (E8) ks[h] = *reinterpret_cast<const f32x4*>(c.k_scale + r.at[h] + 4 * g);
         }
     };
@@ -371,7 +376,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int w = 0; w < VW; w += 4) stream<(VW < 4 ? VW : 4)>(vr[4 * h + i] + w, base + voff + i * row_bytes + w * 4);
+                for (int w = 0; w < VW; w += 4) stream<(VW < 4 ? VW : 4), ONCE>(vr[4 * h + i] + w, base + voff + i * row_bytes + w * 4);
             if constexpr (E8) vs[h] = *reinterpret_cast<const f32x4*>(c.v_scale + r.at[h] + 4 * g);
         }
     };
@@ -758,18 +763,18 @@ AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages, 
     return p;
 }
 
-template <int DT, int CDT, int DP, int NQ>
+template <int DT, int CDT, int DP, int NQ, bool ONCE>
 hipError_t launch_q(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hipStream_t s)
 {
     const dim3 grid((unsigned)((p.groups + 7) / 8 * 8 * p.qtiles));
     if (!p.cut) {
         if constexpr (DP <= 128) {
-            if (p.waves == 8) k_attend<DT, CDT, DP, NQ, 8, false><<<grid, dim3(512), 0, s>>>(c, a, p);
+            if (p.waves == 8) k_attend<DT, CDT, DP, NQ, 8, false, ONCE><<<grid, dim3(512), 0, s>>>(c, a, p);
         }
-        if (p.waves == 4) k_attend<DT, CDT, DP, NQ, 4, false><<<grid, dim3(256), 0, s>>>(c, a, p);
+        if (p.waves == 4) k_attend<DT, CDT, DP, NQ, 4, false, ONCE><<<grid, dim3(256), 0, s>>>(c, a, p);
         return hipGetLastError();
     }
-    k_attend<DT, CDT, DP, NQ, 4, true><<<grid, dim3(256), 0, s>>>(c, a, p);
+    k_attend<DT, CDT, DP, NQ, 4, true, ONCE><<<grid, dim3(256), 0, s>>>(c, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int group = a.q_heads / c.heads, rows = group < NQ * 16 ? group : NQ * 16;
@@ -787,9 +792,11 @@ template <int DT, int CDT, int DP>
 hipError_t launch_d(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hipStream_t s)
 {
     if constexpr (DP <= 128) {
-        if (p.nq == 2) return launch_q<DT, CDT, DP, 2>(c, a, p, s);
+        if (p.nq == 1) return launch_q<DT, CDT, DP, 1, true>(c, a, p, s);       // groups of up to 16: one tile
+        return p.qtiles > 1 ? launch_q<DT, CDT, DP, 2, false>(c, a, p, s) : launch_q<DT, CDT, DP, 2, true>(c, a, p, s);
+    } else {
+        return p.qtiles > 1 ? launch_q<DT, CDT, DP, 1, false>(c, a, p, s) : launch_q<DT, CDT, DP, 1, true>(c, a, p, s);
     }
-    return launch_q<DT, CDT, DP, 1>(c, a, p, s);
 }
 
 template <int DT, int CDT>
