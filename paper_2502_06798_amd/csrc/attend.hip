@@ -39,6 +39,7 @@ namespace apc {
 namespace {
 
 constexpr int TILE = 32;
+constexpr int CUS = 256;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LOWEST = -3.0e38f;      // below every score; finite, so that exp2(-inf - m) is 0
 constexpr float SLACK = 8.f;            // weights stay below 2^8
@@ -219,14 +220,18 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         int64_t total = all.total;
         for (int seq0 = 256; seq0 < a.b; seq0 += 256) total += costs_of(seq0).total;
         total *= c.heads;
-        int64_t share = quotient(total + p.groups - 1, p.groups);
-        share = uniform(share < p.min_share ? p.min_share : share);
+        // Equal shares of at least min_share.  A CU's second workgroup is its
+        // slower one, so a few of them more than there are CUs would only be waited for.
+        int64_t used = quotient(total, p.min_share);
+        used = used < 1 ? 1 : used < p.groups ? used : p.groups;
+        if (used * p.qtiles > CUS) used = used * p.qtiles / CUS * CUS / p.qtiles;
+        used = uniform(used);
         // A cut inside a unit: of a short one moved to its nearer end, of a
         // longer one to the nearest multiple of four tiles in proportion.
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int64_t want = (wg + i) * share;
-            if (want >= total) break;
+            if (wg + i >= used || total == 0) break;
+            const int64_t want = uniform(quotient(total * (wg + i), used));
             const int64_t want_seq = uniform(quotient(want, c.heads));      // want < x heads: want_seq < x
             Costs k = all;
             int64_t ahead = 0;                                  // costs (of one head) of the sequences ahead
@@ -263,7 +268,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                 off_end = off;
             }
         }
-        if (wg * share >= total) {
+        if (wg >= used || total == 0) {
             if (threadIdx.x < 2) rec[threadIdx.x] = 0;
             return;
         }
