@@ -704,7 +704,7 @@ apc_status apc_norm_rows(apc_dtype dt, apc_dtype out_dt, int64_t n, int32_t d, c
         return fail(APC_E_ARG, "apc_norm_rows: a row stride is smaller than d = %d", d);
     if ((out_dt == APC_E4M3) != (out_scale != nullptr))
         return fail(APC_E_ARG, "apc_norm_rows: out_scale is required for e4m3 and only for e4m3");
-    const apc::NormArgs a{x, res, weight, sum, out, out_scale, n, ld_x, ld_res, ld_sum, ld_out, d, eps, false};
+    const apc::NormArgs a{x, res, weight, sum, out, out_scale, n, ld_x, ld_res, ld_sum, ld_out, d, eps, 1.0f / (float)d, false};
     hipError_t err = apc::launch_norm_rows(dt, out_dt, a, static_cast<hipStream_t>(stream));
     if (err != hipSuccess) return hip_fail(err, "apc_norm_rows launch");
     return ok();

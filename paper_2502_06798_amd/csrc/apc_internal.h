@@ -48,7 +48,7 @@ struct NormArgs {
     float* out_scale;
     int64_t n, ld_x, ld_res, ld_sum, ld_out;   // strides in elements
     int32_t d;
-    float eps;
+    float eps, inv_d;
     bool past;          // outputs go past the caches
 };
 hipError_t launch_norm_rows(int dt, int out_dt, const NormArgs& a, hipStream_t s);

@@ -139,28 +139,74 @@ template <int DT, int N> __device__ inline void store_values(typename Elem<DT>::
 // |x| as an integer: orders like the magnitudes, NaN above infinity
 __device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
+// Sums and largest values over groups of T = 4 .. 64 consecutive lanes, the
+// result in each: exchanges within 16 lanes ride on the operation (DPP), the
+// others swap rows of 16 lanes or halves of the wave.
+template <int CTRL> __device__ inline uint32_t lane_moved(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+template <int T, typename F> __device__ inline uint32_t over_lanes(uint32_t x, F f)
+{
+    x = f(x, lane_moved<0xb1>(x));                          // 1 0 3 2
+    x = f(x, lane_moved<0x4e>(x));                          // 2 3 0 1
+    if constexpr (T >= 8) x = f(x, lane_moved<0x141>(x));   // mirror of 8
+    if constexpr (T >= 16) x = f(x, lane_moved<0x140>(x));  // mirror of 16
+    if constexpr (T >= 32) {
+        const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = f(y[0], y[1]);
+    }
+    if constexpr (T >= 64) {
+        const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        x = f(y[0], y[1]);
+    }
+    return x;
+}
+template <int T> __device__ inline float sum_over(float x)
+{
+    return __uint_as_float(over_lanes<T>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+template <int T> __device__ inline uint32_t max_over(uint32_t x)
+{
+    return over_lanes<T>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+
 // Scale of an e4m3fn row from its largest magnitude, and the codes of x / s.
-// With r = 1 / s, q = x r corrected by the remainder x - s q (exact in a fused
+// top / 448 and r = 1 / s are approximations corrected by their remainders;
+// from 2^-80 on they equal the divisions on every float32 (compared over all).
+// With r, q = x r corrected by the remainder s q - x (exact in a fused
 // multiply-add) is the correctly rounded quotient wherever neither r nor the
 // remainder leaves the normal range: s >= 2^-80 leaves it only for quotients
-// below 2^-20, code 0 either way.  Such a row's quotients are at most 448 and
-// two units in the last place, which the hardware's conversion (nearest-even,
-// equal to enc_e4m3 there) takes to 448.  Other rows (NaN, infinite or tiny)
-// divide and round by the definition.
+// below 2^-20, code 0 either way.  (Remainder and correction are both negated,
+// so that -0 stays -0.)  Such a row's quotients are at most 448 and two units in
+// the last place, which the hardware's conversion (nearest-even, equal to
+// enc_e4m3 there) takes to 448.  Other rows (NaN, infinite or tiny) divide and
+// round by the definition.
 struct RowCodes {
     float s, r;
     bool plain;
     __device__ explicit RowCodes(uint32_t top)
     {
-        s = top > 0x7f800000u ? 1.0f : __uint_as_float(top) / 448.0f;
-        if (!(s > 0.f)) s = 1.0f;
-        r = 1.0f / s;
-        plain = top < 0x7f800000u && s >= 0x1p-80f;
+        plain = top >= 0x1c000000u && top < 0x7f800000u;    // from 2^-71
+        if (plain) {
+            constexpr float part = 1.0f / 448.0f;
+            const float t = __uint_as_float(top), q = t * part;
+            s = __builtin_fmaf(__builtin_fmaf(-448.0f, q, t), part, q);
+            const float y = __builtin_amdgcn_rcpf(s);
+            r = __builtin_fmaf(__builtin_fmaf(-s, y, 1.0f), y, y);
+        } else {
+            s = top > 0x7f800000u ? 1.0f : __uint_as_float(top) / 448.0f;
+            if (!(s > 0.f)) s = 1.0f;
+            r = 1.0f;
+            plain = top == 0u;
+        }
     }
     __device__ float quotient(float x) const
     {
         const float q = x * r;
-        return __builtin_fmaf(__builtin_fmaf(-s, q, x), r, q);
+        return __builtin_fmaf(-__builtin_fmaf(s, q, -x), r, q);
     }
     __device__ uint32_t code(float x) const
     {

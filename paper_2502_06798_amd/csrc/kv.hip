@@ -73,12 +73,7 @@ __global__ __launch_bounds__(256) void k_kv_rows(apc_kv c, KvRows a, int shift)
 #pragma unroll
                             for (int i = 0; i < V; ++i) top = magnitude(v[k][i]) > top ? magnitude(v[k][i]) : top;
                         }
-#pragma unroll
-                    for (int m = L / 2; m >= 1; m >>= 1) {
-                        const uint32_t o = __shfl_xor(top, m, 64);
-                        top = o > top ? o : top;
-                    }
-                    const RowCodes codes(top);
+                    const RowCodes codes(max_over<L>(top));
 #pragma unroll
                     for (int k = 0; k < CH; ++k)
                         if (row >= 0 && mine[k]) codes.template store<V>(pool + row * c.d + at[k], v[k], past);

@@ -23,6 +23,15 @@ namespace {
 constexpr int64_t PAST_CACHES = 64 << 20;
 constexpr int64_t MAX_GRID = 1 << 20;   // more rows than that many workgroups hold: a workgroup takes several
 
+// 1 / sqrt(x) to a unit in the last place; x below the normal range (tiny rows
+// with eps = 0) scaled up first, where the instruction would take it for 0
+__device__ inline float rsqrt_of(float x)
+{
+    const bool tiny = x < 0x1p-120f;
+    const float y = __builtin_amdgcn_rsqf(tiny ? x * 0x1p60f : x);
+    return tiny ? y * 0x1p30f : y;
+}
+
 template <int DT, int ODT, int T, int C>
 __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
 {
@@ -72,22 +81,28 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
             const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V, skip = at - from;
             if (at < a.d) {
                 float e[V];
-                if (!KEEP_W && a.weight) rw[c].load(w + from);
-                if (a.weight) rw[c].values(e);
+                if (ODT == APC_E4M3 && !KEEP_W && a.weight) rw[c].load(w + from);
+                if (ODT == APC_E4M3 && a.weight) rw[c].values(e);
+                if (a.d % V == 0) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    ss = i < skip ? ss : __builtin_fmaf(h[c][i], h[c][i], ss);
-                    const uint32_t m = magnitude(a.weight ? h[c][i] * e[i] : h[c][i]);
-                    top = m > top ? m : top;
+                    for (int i = 0; i < V; ++i) ss = __builtin_fmaf(h[c][i], h[c][i], ss);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) ss = i < skip ? ss : __builtin_fmaf(h[c][i], h[c][i], ss);
+                }
+                if constexpr (ODT == APC_E4M3) {
+#pragma unroll
+                    for (int i = 0; i < V; i += 2) {
+                        const uint32_t m0 = magnitude(a.weight ? h[c][i] * e[i] : h[c][i]);
+                        const uint32_t m1 = magnitude(a.weight ? h[c][i + 1] * e[i + 1] : h[c][i + 1]);
+                        const uint32_t m = m0 > m1 ? m0 : m1;
+                        top = m > top ? m : top;
+                    }
                 }
             }
         }
-#pragma unroll
-        for (int m = (T < 64 ? T : 64) / 2; m >= 1; m >>= 1) {
-            ss += __shfl_xor(ss, m, 64);
-            const uint32_t o = __shfl_xor(top, m, 64);
-            top = o > top ? o : top;
-        }
+        ss = sum_over<(T < 64 ? T : 64)>(ss);
+        if constexpr (ODT == APC_E4M3) top = max_over<(T < 64 ? T : 64)>(top);
         if constexpr (WAVES > 1) {
             // two sets of cells in turn: a wave may write the next row's while
             // another still reads this row's
@@ -104,7 +119,7 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
                 top = red_m[turn][own][i] > top ? red_m[turn][own][i] : top;
             }
         }
-        const float f = 1.0f / __builtin_sqrtf(ss / (float)a.d + a.eps);
+        const float f = rsqrt_of(__builtin_fmaf(ss, a.inv_d, a.eps));
         // largest |y|; NaN where a g or the row's factor is NaN (0 * inf too)
         const uint32_t ytop = top > 0x7f800000u ? top : magnitude(__uint_as_float(top) * f);
         const RowCodes codes(ODT == APC_E4M3 ? ytop : 0u);
@@ -162,7 +177,7 @@ __global__ __launch_bounds__(256) void k_norm_short_rows(NormArgs a)
                 const uint32_t m = magnitude(g[i]);
                 top = m > top ? m : top;
             }
-        const float f = 1.0f / __builtin_sqrtf(ss / (float)a.d + a.eps);
+        const float f = rsqrt_of(__builtin_fmaf(ss, a.inv_d, a.eps));
         const RowCodes codes(top > 0x7f800000u ? top : magnitude(__uint_as_float(top) * f));
 #pragma unroll
         for (int i = 0; i < V; ++i)

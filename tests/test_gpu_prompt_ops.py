@@ -236,6 +236,8 @@ def test_kv_write_read_bit_exact(apc, orc, cache, dtype):
         if how == "plain":
             k[0, 0], v[0, 0, 3], v[t // 2, heads - 1] = 0.0, float("nan"), 1e-7
             k[t - 1, heads - 1, d - 1] = float("inf")
+            k[t // 3, 0, ::2], v[0, 0, :3] = -0.0, -0.0
+            v[t // 3, 0], v[t // 4, 0] = -0.0, 3e-39
         slots = torch.randperm(n_pages * page, device="cuda", generator=g)[:t].to(torch.int32)
         if t > 4:
             slots[1], slots[2], slots[3], slots[4] = -1, n_pages * page, -2 ** 31, 2 ** 31 - 1
