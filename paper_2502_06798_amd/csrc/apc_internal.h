@@ -78,6 +78,7 @@ struct AttendPlan {
     int32_t groups;      // workgroups (for each query tile) that share the tiles of all sequences and heads
     int32_t min_share;   // tiles that a workgroup takes at least, as long as there are as many
     int32_t snap;        // sequences of up to so many tiles are not cut
+    bool once;           // keys and values pass the caches by
     bool cut;            // some could be longer: stretches of all tiles, joined; else whole units
 };
 size_t attend_workspace(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages);

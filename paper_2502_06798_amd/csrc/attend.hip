@@ -29,7 +29,12 @@
 // Bound by memory: every key and value is read once, into the registers that
 // the matrix instructions take.  A wave's next tile, of the same unit or of the
 // workgroup's next one, is on its way while this one is computed, joined with
-// the other waves' and stored.
+// the other waves' and stored.  64 sequences of 16,384 to 32,768 tokens, 4 x 8
+// heads of 128, e4m3: 525 us, 6.3 TB/s, what streaming reads reach on this
+// card; 256 of 100 to 2,048 over bf16: 190 us, 6.0; one of 131,072 over e4m3: 50
+// us and 5.5 in the join (its workgroups end from 31 to 49 us: a CU's older
+// waves go first).  A call of little work is its latency: some 2 us to launch,
+// 2 for its share, 2 to 3 for its first keys, 2 for each further tile of a wave.
 #include "apc_internal.h"
 #include "convert.h"
 
@@ -79,11 +84,12 @@ template <bool BF, bool HIGH> __device__ inline uint32_t from_e4m3(uint32_t w)
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
 }
 
-// N dwords of keys or values.  ONCE: read by one workgroup only, so marked not
-// to displace what is in the caches (256 sequences over bf16: 199 us, 209
-// without; 64 long ones: 578, 598); but where several workgroups have the query
-// heads of one key-value head, the second finds what the first read (64
-// sequences, 128 query heads on one of 128, bf16: 162 us, 234 past the caches).
+// N dwords of keys or values.  ONCE: marked not to displace what is in the
+// caches (256 sequences of 100 to 2,048 tokens, bf16: 190 us, 212 without; 64 of
+// 16,384 to 32,768, e4m3: 530 and 570).  Not so where the next call may find them
+// there (16 of 1,024, bf16: 15.6 us, 21.1 marked), and where several workgroups
+// have the query heads of one key-value head, the second of which finds what the
+// first read (64 sequences, 128 query heads on one of 128, bf16: 161 us, 234 marked).
 template <int N, bool ONCE> __device__ inline void stream(uint32_t* to, const uint8_t* from)
 {
     if constexpr (N == 1) {
@@ -159,7 +165,7 @@ __device__ inline float* partial_stats(const AttendArgs& a, const AttendPlan& p,
     return partial_sums(a, p) + (int64_t)p.groups * p.qtiles * 2 * rows * dp;
 }
 
-// CUT: stretches of the row of all tiles; else whole units.  ONCE: one query tile a group
+// CUT: stretches of the row of all tiles; else whole units.  ONCE: see stream()
 template <int DT, int CDT, int DP, int NQ, int WAVES, bool CUT, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv c, AttendArgs a, AttendPlan p)
 {
@@ -743,6 +749,11 @@ int stretches(const apc_kv& c, int qtiles)
     const int groups = padded(c.d) > 128 ? 256 : c.d * elem_bytes(c.dt) <= 64 ? 1024 : 512;
     return groups / qtiles > 0 ? groups / qtiles : 1;
 }
+// Calls that could read as much find little of it again in the 256 MB
+// last-level cache, even where a next call reads the same keys and values
+// (three caches in turn, 24 x 8 units of 1,024 tokens over bf16, 101 MB: 20.8 us,
+// 22.3 marked; 32 x 8, 134 MB: 26.9 and 25.0).
+constexpr int64_t ONCE_BYTES = 100 << 20;
 constexpr int64_t UNCUT_GROUPS = 1 << 16;
 AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages, int32_t window)
 {
@@ -765,6 +776,7 @@ AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages, 
         groups = shares < most ? shares : most;
     }
     p.groups = (int32_t)groups;
+    p.once = p.qtiles == 1 && units * unit_bytes >= ONCE_BYTES;
     return p;
 }
 
@@ -797,11 +809,9 @@ template <int DT, int CDT, int DP>
 hipError_t launch_d(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hipStream_t s)
 {
     if constexpr (DP <= 128) {
-        if (p.nq == 1) return launch_q<DT, CDT, DP, 1, true>(c, a, p, s);       // groups of up to 16: one tile
-        return p.qtiles > 1 ? launch_q<DT, CDT, DP, 2, false>(c, a, p, s) : launch_q<DT, CDT, DP, 2, true>(c, a, p, s);
-    } else {
-        return p.qtiles > 1 ? launch_q<DT, CDT, DP, 1, false>(c, a, p, s) : launch_q<DT, CDT, DP, 1, true>(c, a, p, s);
+        if (p.nq == 2) return p.once ? launch_q<DT, CDT, DP, 2, true>(c, a, p, s) : launch_q<DT, CDT, DP, 2, false>(c, a, p, s);
     }
+    return p.once ? launch_q<DT, CDT, DP, 1, true>(c, a, p, s) : launch_q<DT, CDT, DP, 1, false>(c, a, p, s);
 }
 
 template <int DT, int CDT>
