@@ -5,8 +5,8 @@
 // unit with EXTRA more, for what a unit costs besides its tiles) and every
 // workgroup takes an equal stretch of it, so that ragged lengths leave none with
 // more than its share; a unit that several workgroups share leaves partial
-// results, which k_attend_join joins.  Otherwise a workgroup takes a unit at a
-// time.  For each unit it computes up to NQ x 16 of the query heads
+// results, which k_attend_join joins.  Otherwise a workgroup, of one wave where
+// there are many short units, takes a unit at a time.  For each unit it computes up to NQ x 16 of the query heads
 // that share the key-value head, wave w of WAVES every WAVES-th tile.
 //
 // A tile, per wave, in matrix instructions of 16 x 16 x 32:
@@ -602,7 +602,12 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                         const float f = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
                         for (int i = 0; i < PER; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
-                        store_values<DT, PER>(static_cast<T*>(a.out) + cur.seq * a.out_row + qrow * a.out_head + d0 + dcol, v);
+                        T* const to = static_cast<T*>(a.out) + cur.seq * a.out_row + qrow * a.out_head + d0 + dcol;
+                        // d is a multiple of 16: a thread's elements, where they are more, can end past it
+                        constexpr int ST = PER < 16 ? PER : 16;
+#pragma unroll
+                        for (int i = 0; i < PER; i += ST)
+                            if (d0 + dcol + i < c.d) store_values<DT, ST>(to + i, v + i);
                         if (a.lse && d0 + dcol == 0)
                             a.lse[(int64_t)cur.seq * a.q_heads + qrow] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
                     } else {
@@ -749,6 +754,18 @@ int stretches(const apc_kv& c, int qtiles)
     const int groups = padded(c.d) > 128 ? 256 : c.d * elem_bytes(c.dt) <= 64 ? 1024 : 512;
     return groups / qtiles > 0 ? groups / qtiles : 1;
 }
+// One wave has a unit to itself, and nothing to join, where the unit is a tile,
+// or where there are enough short units for every SIMD: of eight tiles at most
+// (256 x 8 units of 128 tokens, bf16, heads of 128: 25.7 us, 28.7 with four
+// waves; 149 x 11 of one to three, e4m3: 9.7 and 15.3), or of 32 with wide heads,
+// whose registers leave a CU a single workgroup of four (256 x 8 of 512, heads of
+// 256, e4m3: 99.8 us and 123.4; bf16, 1 MB a unit: 182 us, 206 in stretches).
+// Narrower heads have no gain there, and lose where the lengths differ (256 x 12
+// of 1 to 500 tokens, heads of 64: 43.4 us and 40.2).
+bool one_wave(int d, int64_t units, int64_t seen)
+{
+    return seen <= 1 || (units >= 1024 && seen <= 8) || (padded(d) > 128 && units >= 2048 && seen <= 32);
+}
 // Calls that could read as much find little of it again in the 256 MB
 // last-level cache, even where a next call reads the same keys and values
 // (three caches in turn, 24 x 8 units of 1,024 tokens over bf16, 101 MB: 20.8 us,
@@ -768,8 +785,9 @@ AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages, 
     // a window bounds the tiles that are seen, too
     const int64_t seen = window > 0 && window / TILE + 2 < tiles ? window / TILE + 2 : tiles;
     const int64_t unit_bytes = seen * TILE * 2 * c.d * elem_bytes(c.dt);
-    p.waves = padded(c.d) <= 128 && units * p.qtiles <= WIDE_UNITS && seen > 4 ? 8 : 4;
-    p.cut = unit_bytes > (p.waves == 8 && units >= WIDE_UNITS / 2 ? WHOLE_UNIT_MANY : WHOLE_UNIT);
+    p.waves = padded(c.d) <= 128 && units * p.qtiles <= WIDE_UNITS && seen > 4 ? 8
+              : one_wave(c.d, units * p.qtiles, seen) ? 1 : 4;
+    p.cut = p.waves != 1 && unit_bytes > (p.waves == 8 && units >= WIDE_UNITS / 2 ? WHOLE_UNIT_MANY : WHOLE_UNIT);
     int64_t groups = units < UNCUT_GROUPS ? units : UNCUT_GROUPS;
     if (p.cut) {
         const int64_t shares = (units * (seen + EXTRA) + MIN_SHARE - 1) / MIN_SHARE, most = stretches(c, p.qtiles);
@@ -788,6 +806,7 @@ hipError_t launch_q(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, h
         if constexpr (DP <= 128) {
             if (p.waves == 8) k_attend<DT, CDT, DP, NQ, 8, false, ONCE><<<grid, dim3(512), 0, s>>>(c, a, p);
         }
+        if (p.waves == 1) k_attend<DT, CDT, DP, NQ, 1, false, ONCE><<<grid, dim3(64), 0, s>>>(c, a, p);
         if (p.waves == 4) k_attend<DT, CDT, DP, NQ, 4, false, ONCE><<<grid, dim3(256), 0, s>>>(c, a, p);
         return hipGetLastError();
     }

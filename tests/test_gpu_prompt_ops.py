@@ -478,6 +478,29 @@ def test_attend_many_sequences(apc, orc, cache, dtype, b, heads, group, d, cap, 
     assert (out == 0).all() and torch.isneginf(lse).all()
 
 
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("b,heads,group,d,page,most", [(1200, 1, 3, 16, 16, 32), (130, 8, 5, 80, 32, 256), (130, 8, 20, 128, 64, 256),
+                                                       (520, 2, 1, 64, 16, 200), (264, 4, 40, 64, 16, 100), (130, 8, 2, 192, 32, 256),
+                                                       (130, 16, 4, 256, 64, 960), (1030, 2, 17, 256, 16, 70)])
+def test_attend_a_wave_to_a_unit(apc, orc, cache, dtype, b, heads, group, d, page, most):
+    """Many (sequence, head) pairs of a few tiles each, the sequences on a pool of shared pages."""
+    say(f"attend wave a unit {dtype} over {cache} b={b} heads={heads} group={group} d={d} page={page} most={most}")
+    rows, g = 16, gen(b + d)
+    pool, few, q = make_attend(b + d, rows, heads, group, d, page, -(-most // page), cache, dtype)
+    q = torch.randn((b, heads * group, d), device="cuda", generator=g).to(q.dtype)
+    table = few[torch.randint(0, rows, (b,), device="cuda", generator=g)].contiguous()
+    lens = torch.randint(0, most + 1, (b,), device="cuda", generator=g).to(torch.int32)
+    lens[b // 5:b // 4], lens[b // 2], lens[-1] = 0, most, most
+    at = torch.cat([torch.arange(0, 8), torch.arange(b // 5 - 2, b // 5 + 2), torch.arange(b // 2 - 2, b // 2 + 2),
+                    torch.arange(b - 12, b)]).cuda()
+    for window in (0, 50):
+        out, lse = run_attend(apc, pool, table, q, lens, d ** -0.5, window)
+        check_attend(orc, cache, dtype, pool, table[at], q[at], lens[at], d ** -0.5, window, out[at], lse[at])
+        assert torch.equal(torch.isneginf(lse).all(dim=1), lens == 0) and (out[lens > 0].float().abs().amax(dim=2) > 0).all()
+        again = run_attend(apc, pool, table, q, lens, d ** -0.5, window)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
 def test_attend_more_units_than_workgroups(apc, orc):
     """Short sequences in more (sequence, head) pairs than a launch has workgroups for."""
     b, heads, d, page = 9000, 8, 16, 16
