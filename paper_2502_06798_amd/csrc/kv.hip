@@ -7,7 +7,7 @@
 // carries 64 / L rows.  A lane keeps the same head and goes on to U tokens, all
 // of whose loads are in flight before the first is converted.  Bound by memory:
 // the rows in and the stored bytes out, once each.  65,536 tokens x 8 x 128
-// bf16 to e4m3 79 us, 5.0 TB/s; 100,003 of them back to bf16 115 us, 5.4 TB/s (a
+// bf16 to e4m3 76 us, 5.2 TB/s; 100,003 of them back to bf16 112 us, 5.5 TB/s (a
 // large copy reaches 4.6).
 #include "apc_internal.h"
 #include "convert.h"
@@ -36,12 +36,19 @@ __global__ __launch_bounds__(256) void k_kv_rows(apc_kv c, KvRows a, int shift)
     for (int k = 0; k < CH; ++k) at[k] = (k * L + threadIdx.x % L) * V, mine[k] = at[k] < c.d;
     const int64_t slots = c.n_pages << shift;
     // Large calls go past the caches, where nobody would find their output again
-    // (100,003 tokens x 8 x 128 from e4m3 to bf16: 115 us, 123 without; 65,536
-    // bf16 to bf16: 95 and 104), if rows are whole halves of lines (parts of
-    // them, 17,549 x 15 x 16 to e4m3: 21 us, 16 without).
-    const bool past = U > 1 && c.d * (int)sizeof(typename Elem<WRITE ? CDT : DT>::T) % 64 == 0;
+    // (100,003 tokens x 8 x 128 from e4m3 to bf16: 112 us, 120 without; 65,536
+    // bf16 to bf16: 93 and 100), but for pages' rows that are no whole halves of
+    // lines (65,536 x 15 x 80 bf16: 137 us, 121 without).
+    const bool past = U > 1 && (!WRITE || c.d * (int)sizeof(S) % 64 == 0);
     const int32_t rows = 2 * c.heads;           // of a token: every head's key, then every head's value
-    const int64_t unit0 = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L, units = (a.t + U - 1) / U * rows;
+    // Workgroups go round the eight L2s: of a large call, each L2 has RUN
+    // neighbours, which share the lines of the scales and the pages' rows (65,536
+    // x 8 x 128 to e4m3: 75.8 us, 79.7 with one; 100,003 of them read: 111.9 and
+    // 115.9).
+    constexpr uint32_t RUN = U > 1 ? 32 : 1, SET = 8 * RUN;
+    const uint32_t in_sets = gridDim.x / SET * SET, set = blockIdx.x / SET * SET, at_set = blockIdx.x % SET;
+    const uint32_t wg = blockIdx.x < in_sets ? set + at_set % 8 * RUN + at_set / 8 : blockIdx.x;
+    const int64_t unit0 = (int64_t)wg * (256 / L) + threadIdx.x / L, units = (a.t + U - 1) / U * rows;
     for (int64_t unit = unit0; unit < units; unit += (int64_t)gridDim.x * (256 / L)) {
         // t * heads < 2^31, so there are fewer than 2^32 units
         const uint32_t token = (uint32_t)unit / (uint32_t)rows;
@@ -127,12 +134,15 @@ void launch_l(const apc_kv& c, const KvRows& a, hipStream_t s)
     int shift = 0;
     while ((1 << shift) < c.page) ++shift;
     const int64_t rows = a.t * 2 * c.heads;
-    // four tokens a lane where the rows fill the chip's 2,048 lanes a CU all the
-    // same (65,536 x 8 x 128 to e4m3: 79 us, 82 to 89 with two, 82 with eight)
-    const int u = rows * L >= 4 * 256 * 2048 ? 4 : 1;
+    // two tokens a lane, or four of wide e4m3 rows, where four would fill the
+    // chip's 2,048 lanes a CU all the same (65,536 x 8 x 128 to e4m3: 75.8 us, 77
+    // to 85 with two, 80 with eight; 65,536 x 8 x 128 bf16 read: 92 with two, 95
+    // with four; 77,777 x 20 x 32 to e4m3: 72 and 79)
+    constexpr int MANY = CDT == APC_E4M3 && L >= 16 ? 4 : 2;
+    const int u = rows * L >= 4 * 256 * 2048 ? MANY : 1;
     const int64_t groups = ((a.t + u - 1) / u * 2 * c.heads + 256 / L - 1) / (256 / L);
     const dim3 grid((unsigned)(groups < MAX_GRID ? groups : MAX_GRID)), block(256);
-    if (u == 4) k_kv_rows<WRITE, DT, CDT, L, 4><<<grid, block, 0, s>>>(c, a, shift);
+    if (u == MANY) k_kv_rows<WRITE, DT, CDT, L, MANY><<<grid, block, 0, s>>>(c, a, shift);
     else k_kv_rows<WRITE, DT, CDT, L, 1><<<grid, block, 0, s>>>(c, a, shift);
 }
 

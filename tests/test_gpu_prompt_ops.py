@@ -292,6 +292,38 @@ def test_kv_empty_and_many(apc, orc):
     assert np.array_equal(f64(ko[at]), f64(torch.from_numpy(want).to(torch.bfloat16)))
 
 
+@pytest.mark.parametrize("cache", ["f16", "bf16", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("t,heads,d", [(8195, 32, 32), (8197, 17, 64), (4099, 16, 80), (2051, 17, 176)])
+def test_kv_large_calls_are_small_calls(apc, cache, dtype, t, heads, d):
+    """Calls whose lanes go on to several tokens leave the bits that calls of 300 tokens leave, slots outside the pool among them."""
+    say(f"kv large {dtype}->{cache} t={t} heads={heads} d={d}")
+    page, g = 64, gen(t + d)
+    n_pages = t // page + 3
+    x = (torch.randn((t, 2 * heads, d), device="cuda", generator=g)
+         * torch.exp(torch.randn((t, 2 * heads, 1), device="cuda", generator=g) * 3)).to(TORCH[dtype])
+    k, v = x[:, :heads], x[:, heads:]
+    slots = torch.randperm(n_pages * page, device="cuda", generator=g)[:t].to(torch.int32)
+    slots[::7] = -1
+    slots[t - 2] = n_pages * page
+    one, many = (apc.KvCache(*make_pool(n_pages, heads, page, d, cache)) for _ in range(2))
+    apc.apc_kv_write(one, k, v, slots)
+    for i in range(0, t, 300):
+        apc.apc_kv_write(many, k[i:i + 300], v[i:i + 300], slots[i:i + 300])
+    for a, b in zip((one.k, one.v, one.k_scale, one.v_scale), (many.k, many.v, many.k_scale, many.v_scale)):
+        assert a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    got, want = (torch.full((2, t, heads, d), 5.0, device="cuda").to(TORCH[dtype]) for _ in range(2))
+    apc.apc_kv_read(one, slots, got[0], got[1])
+    for i in range(0, t, 300):
+        apc.apc_kv_read(one, slots[i:i + 300], want[0, i:i + 300], want[1, i:i + 300])
+    assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
+    out = (slots < 0) | (slots >= n_pages * page)
+    top = torch.stack([k, v])[:, ~out].float().abs().amax(dim=3)
+    some = torch.isfinite(top) & (top > 1e-4)                # a half's rows reach infinity here and there
+    assert some.float().mean() > 0.9
+    assert (got[:, out] == 0).all() and (got[:, ~out].float().abs().amax(dim=3)[some] > 0).all()
+
+
 # ---- attention ---------------------------------------------------------------
 
 def make_attend(seed, b, heads, group, d, page, max_pages, cache, dtype, extra=3, spread=1.0):
