@@ -3,7 +3,9 @@
 The per-batch step of prompt-aware scheduling for diffusion serving with
 approximate caching: nearest cached prompts (cosine top-k), optimal skip
 level, capacity-constrained placement on model instances, and the gather of
-the cached latents.  The compute lives in hand-written HIP kernels behind the
+the cached latents; and the operators of a text model that reads the prompts
+token by token (norm of rows, paged key-value cache, attention over it), whose
+embeddings the first step takes.  The compute lives in hand-written HIP kernels behind the
 C ABI of include/apc.h; this package is its thin Python binding plus the
 seeded synthetic workload generator (synth).
 """
