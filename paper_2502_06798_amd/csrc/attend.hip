@@ -772,6 +772,14 @@ bool one_wave(int d, int64_t units, int64_t seen)
 // 22.3 marked; 32 x 8, 134 MB: 26.9 and 25.0).
 constexpr int64_t ONCE_BYTES = 100 << 20;
 constexpr int64_t UNCUT_GROUPS = 1 << 16;
+int64_t tiles_of(const apc_kv& c, int64_t max_pages) { return (max_pages * c.page + TILE - 1) / TILE; }
+int64_t bytes_of(const apc_kv& c, int64_t tiles) { return tiles * TILE * 2 * c.d * elem_bytes(c.dt); }
+// Stretches of units of so many tiles: no fewer for more units or tiles
+int32_t cut_groups(const apc_kv& c, int64_t units, int64_t tiles, int qtiles)
+{
+    const int64_t shares = (units * (tiles + EXTRA) + MIN_SHARE - 1) / MIN_SHARE, most = stretches(c, qtiles);
+    return (int32_t)(shares < most ? shares : most);
+}
 AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages, int32_t window)
 {
     AttendPlan p{};
@@ -781,19 +789,14 @@ AttendPlan plan(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages, 
     p.qtiles = (group + 16 * p.nq - 1) / (16 * p.nq);
     p.snap = SNAP;
     p.min_share = MIN_SHARE;
-    const int64_t units = (int64_t)b * c.heads, tiles = (((int64_t)max_pages << p.shift) + TILE - 1) / TILE;
+    const int64_t units = (int64_t)b * c.heads, tiles = tiles_of(c, max_pages);
     // a window bounds the tiles that are seen, too
     const int64_t seen = window > 0 && window / TILE + 2 < tiles ? window / TILE + 2 : tiles;
-    const int64_t unit_bytes = seen * TILE * 2 * c.d * elem_bytes(c.dt);
+    const int64_t unit_bytes = bytes_of(c, seen);
     p.waves = padded(c.d) <= 128 && units * p.qtiles <= WIDE_UNITS && seen > 4 ? 8
               : one_wave(c.d, units * p.qtiles, seen) ? 1 : 4;
     p.cut = p.waves != 1 && unit_bytes > (p.waves == 8 && units >= WIDE_UNITS / 2 ? WHOLE_UNIT_MANY : WHOLE_UNIT);
-    int64_t groups = units < UNCUT_GROUPS ? units : UNCUT_GROUPS;
-    if (p.cut) {
-        const int64_t shares = (units * (seen + EXTRA) + MIN_SHARE - 1) / MIN_SHARE, most = stretches(c, p.qtiles);
-        groups = shares < most ? shares : most;
-    }
-    p.groups = (int32_t)groups;
+    p.groups = p.cut ? cut_groups(c, units, seen, p.qtiles) : (int32_t)(units < UNCUT_GROUPS ? units : UNCUT_GROUPS);
     p.once = p.qtiles == 1 && units * unit_bytes >= ONCE_BYTES;
     return p;
 }
@@ -847,8 +850,12 @@ hipError_t launch(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, hip
 
 size_t attend_workspace(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages)
 {
-    const AttendPlan p = plan(c, b, q_heads, max_pages, 0);
-    if (!p.cut) return 0;
+    // what the call would ask if its units were cut, where the units of a smaller
+    // batch over the same table, or with a window, could be
+    AttendPlan p = plan(c, b, q_heads, max_pages, 0);
+    const int64_t tiles = tiles_of(c, max_pages);
+    if (bytes_of(c, tiles) <= WHOLE_UNIT) return 0;
+    p.groups = cut_groups(c, (int64_t)b * c.heads, tiles, p.qtiles);
     const int group = q_heads / c.heads, rows = group < p.nq * 16 ? group : p.nq * 16;
     return (size_t)(rec_ints(p) + (int64_t)p.groups * p.qtiles * 2 * rows * (padded(c.d) + 2)) * sizeof(float);
 }

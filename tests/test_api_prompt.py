@@ -129,6 +129,25 @@ def test_attend_workspace_never_falls(lib):
                         last = n.value
 
 
+@pytest.mark.parametrize("dt,ks", [(F16, 0), (E4M3, 0x100000)])
+@pytest.mark.parametrize("heads,d,page", [(8, 128, 64), (8, 256, 64), (16, 192, 32), (12, 64, 16), (200, 128, 16), (2, 32, 1024)])
+@pytest.mark.parametrize("group", [1, 8, 24])
+def test_attend_workspace_serves_every_smaller_call(lib, dt, ks, heads, d, page, group):
+    """No batch and no table within a call's asks for more, where the kernel that takes it changes with either."""
+    kv = ctypes.byref(_kv(dt=dt, heads=heads, d=d, page=page, ks=ks, vs=ks))
+    tables = [t * 16 // page for t in range(0, 300, 3) if t * 16 % page == 0] + [2000]
+    above = [0] * len(tables)
+    for b in (1, 2, 10, 15, 16, 17, 31, 32, 33, 63, 64, 127, 128, 129, 255, 256, 300, 1023, 1024, 2048):
+        if b * heads * group > 1 << 23:                       # refused
+            break
+        left = 0
+        for i, mp in enumerate(tables):
+            n = ctypes.c_size_t()
+            assert lib.apc_attend_workspace(kv, b, heads * group, mp, ctypes.byref(n)) == 0
+            assert n.value >= above[i] and n.value >= left, (b, mp)
+            above[i] = left = n.value
+
+
 def test_binding_refuses_host_and_misshapen_tensors():
     import torch
 

@@ -533,6 +533,29 @@ def test_attend_a_wave_to_a_unit(apc, orc, cache, dtype, b, heads, group, d, pag
         assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
 
 
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("b,heads,group,d,page,cap", [(260, 8, 2, 256, 64, 960), (20, 8, 4, 128, 64, 960), (300, 8, 24, 256, 16, 960)])
+def test_attend_workspace_of_a_larger_batch(apc, orc, cache, dtype, b, heads, group, d, page, cap):
+    """One workspace, made for the largest batch and table, with every smaller call's: uncut units next to cut ones."""
+    say(f"attend one workspace {dtype} over {cache} b={b} heads={heads} d={d}")
+    rows, g = 6, gen(b + d)
+    pool, few, _ = make_attend(b + d, rows, heads, group, d, page, cap // page, cache, dtype)
+    c = apc.KvCache(*pool)
+    ws = apc.attend_workspace_tensor(c, b, heads * group, cap // page)
+    for n in (b, 100, 15, 3, 1):
+        if n > b:
+            continue
+        q = torch.randn((n, heads * group, d), device="cuda", generator=g).to(TORCH[dtype])
+        table = few[torch.arange(n, device="cuda") % rows].contiguous()
+        lens = torch.randint(cap // 2, cap + 1, (n,), device="cuda", generator=g).to(torch.int32)
+        for window in (0, 700):
+            out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+            ws.fill_(0xff)
+            apc.apc_attend(c, q, table, lens, d ** -0.5, out, ws, lse, window)
+            torch.cuda.synchronize()
+            check_attend(orc, cache, dtype, pool, table[-4:], q[-4:], lens[-4:], d ** -0.5, window, out[-4:], lse[-4:])
+
+
 def test_attend_more_units_than_workgroups(apc, orc):
     """Short sequences in more (sequence, head) pairs than a launch has workgroups for."""
     b, heads, d, page = 9000, 8, 16, 16
