@@ -585,41 +585,42 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                     }
                 }
                 __syncthreads();
+                // every thread sums and only the stores are some threads': copies of the next round's registers,
+                // where the compiler makes any here, would be lost in the threads that a branch leaves out
                 const int qh = (qt * NQ + n) * 16 + hrow;
-                if (qh < group && d0 + dcol < c.d) {
-                    float top = LOWEST, sum = 0.f, v[PER] = {};
+                const bool mine = qh < group && d0 + dcol < c.d;
+                float top = LOWEST, sum = 0.f, v[PER] = {};
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) top = __builtin_fmaxf(top, ml[turn][w][n * 16 + hrow][0]);
+                for (int w = 0; w < WAVES; ++w) top = __builtin_fmaxf(top, ml[turn][w][n * 16 + hrow][0]);
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) {
-                        const float f = __builtin_amdgcn_exp2f(ml[turn][w][n * 16 + hrow][0] - top);
-                        sum = __builtin_fmaf(f, ml[turn][w][n * 16 + hrow][1], sum);
+                for (int w = 0; w < WAVES; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(ml[turn][w][n * 16 + hrow][0] - top);
+                    sum = __builtin_fmaf(f, ml[turn][w][n * 16 + hrow][1], sum);
 #pragma unroll
-                        for (int i = 0; i < PER; ++i) v[i] = __builtin_fmaf(f, part[w][hrow][dcol + i], v[i]);
-                    }
-                    if (!CUT || whole_unit) {
-                        const int64_t qrow = (int64_t)cur.head * group + qh;
-                        const float f = sum == 0.f ? 0.f : 1.0f / sum;
+                    for (int i = 0; i < PER; ++i) v[i] = __builtin_fmaf(f, part[w][hrow][dcol + i], v[i]);
+                }
+                if (!CUT || whole_unit) {
+                    const int64_t qrow = (int64_t)cur.head * group + qh;
+                    const float f = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-                        for (int i = 0; i < PER; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
-                        T* const to = static_cast<T*>(a.out) + cur.seq * a.out_row + qrow * a.out_head + d0 + dcol;
-                        // d is a multiple of 16: a thread's elements, where they are more, can end past it
-                        constexpr int ST = PER < 16 ? PER : 16;
+                    for (int i = 0; i < PER; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
+                    T* const to = static_cast<T*>(a.out) + cur.seq * a.out_row + qrow * a.out_head + d0 + dcol;
+                    // d is a multiple of 16: a thread's elements, where they are more, can end past it
+                    constexpr int ST = PER < 16 ? PER : 16;
 #pragma unroll
-                        for (int i = 0; i < PER; i += ST)
-                            if (d0 + dcol + i < c.d) store_values<DT, ST>(to + i, v + i);
-                        if (a.lse && d0 + dcol == 0)
-                            a.lse[(int64_t)cur.seq * a.q_heads + qrow] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
-                    } else {
-                        const int64_t slot = (((int64_t)wg * p.qtiles + qt) * 2 + parts) * rows + n * 16 + hrow;
-                        float* po = partial_sums(a, p) + slot * DP + d0 + dcol;
+                    for (int i = 0; i < PER; i += ST)
+                        if (mine && d0 + dcol + i < c.d) store_values<DT, ST>(to + i, v + i);
+                    if (a.lse && mine && d0 + dcol == 0)
+                        a.lse[(int64_t)cur.seq * a.q_heads + qrow] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+                } else if (mine) {
+                    const int64_t slot = (((int64_t)wg * p.qtiles + qt) * 2 + parts) * rows + n * 16 + hrow;
+                    float* po = partial_sums(a, p) + slot * DP + d0 + dcol;
 #pragma unroll
-                        for (int i = 0; i < PER; i += 4) *reinterpret_cast<f32x4*>(po + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
-                        if (d0 + dcol == 0) {
-                            float* pm = partial_stats(a, p, rows, DP) + slot * 2;
-                            pm[0] = top;
-                            pm[1] = sum;
-                        }
+                    for (int i = 0; i < PER; i += 4) *reinterpret_cast<f32x4*>(po + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+                    if (d0 + dcol == 0) {
+                        float* pm = partial_stats(a, p, rows, DP) + slot * 2;
+                        pm[0] = top;
+                        pm[1] = sum;
                     }
                 }
             }

@@ -556,6 +556,19 @@ def test_attend_workspace_of_a_larger_batch(apc, orc, cache, dtype, b, heads, gr
             check_attend(orc, cache, dtype, pool, table[-4:], q[-4:], lens[-4:], d ** -0.5, window, out[-4:], lse[-4:])
 
 
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("b,heads,group,d,page,lens", [(4, 1, 24, 256, 16, [0, 1, 37, 500]), (3, 2, 33, 192, 64, [4100, 2, 1500]),
+                                                       (2, 1, 64, 144, 32, [2049, 700]), (1, 1, 32, 256, 128, [9000])])
+def test_attend_many_heads_of_wide_rows(apc, orc, cache, dtype, b, heads, group, d, page, lens):
+    """More than 16 query heads to a key-value head with heads wider than 128: uncut, cut, several query tiles."""
+    say(f"attend wide {dtype} over {cache} b={b} heads={heads} group={group} d={d} lens={lens}")
+    pool, table, q = make_attend(d + group, b, heads, group, d, page, -(-max(lens) // page), cache, dtype)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    for window in (0, 333):
+        out, lse = run_attend(apc, pool, table, q, n, d ** -0.5, window)
+        check_attend(orc, cache, dtype, pool, table, q, n, d ** -0.5, window, out, lse)
+
+
 def test_attend_more_units_than_workgroups(apc, orc):
     """Short sequences in more (sequence, head) pairs than a launch has workgroups for."""
     b, heads, d, page = 9000, 8, 16, 16
