@@ -227,10 +227,11 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         for (int seq0 = 256; seq0 < a.b; seq0 += 256) total += costs_of(seq0).total;
         total *= c.heads;
         // Equal shares of at least min_share.  A CU's second workgroup is its
-        // slower one, so a few of them more than there are CUs would only be waited for.
+        // slower one, so a few of them more than there are CUs would only be waited for
+        // (one stretch stays one, with more query tiles than CUs too).
         int64_t used = quotient(total, p.min_share);
         used = used < 1 ? 1 : used < p.groups ? used : p.groups;
-        if (used * p.qtiles > CUS) used = used * p.qtiles / CUS * CUS / p.qtiles;
+        if (used > 1 && used * p.qtiles > CUS) used = used * p.qtiles / CUS * CUS / p.qtiles;
         used = uniform(used);
         // A cut inside a unit: of a short one moved to its nearer end, of a
         // longer one to the nearest multiple of four tiles in proportion.
