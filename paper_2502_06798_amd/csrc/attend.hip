@@ -194,10 +194,11 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         for (int seq = wg; seq < a.b; seq += p.groups) {
             if (span_of(seq).tiles > 0) continue;
             const int h0 = qt * NQ * 16, n = group - h0 < NQ * 16 ? group - h0 : NQ * 16;
-            for (int i = threadIdx.x; i < c.heads * n * c.d; i += 64 * WAVES) {
-                const int d = i % c.d, h = i / c.d / n * group + h0 + i / c.d % n;
-                static_cast<T*>(a.out)[seq * a.out_row + h * a.out_head + d] = 0;
-                if (a.lse && d == 0) a.lse[(int64_t)seq * a.q_heads + h] = -INFINITY;
+            for (int i = wave; i < c.heads * n; i += WAVES) {   // a head a wave: all elements pass 32 bits
+                const int h = i / n * group + h0 + i % n;
+                T* const to = static_cast<T*>(a.out) + seq * a.out_row + h * a.out_head;
+                for (int d = lane; d < c.d; d += 64) to[d] = 0;
+                if (a.lse && lane == 0) a.lse[(int64_t)seq * a.q_heads + h] = -INFINITY;
             }
         }
         // The stretch, found by every wave for itself: a lane has four of every

@@ -31,3 +31,17 @@ def test_attend_more_query_tiles_than_compute_units(apc, orc, cache, dtype, grou
     assert (out[1] == 0).all() and not (out[::2] == 7.0).all(dim=2).any() and not (lse == 7.0).any()
     at = torch.tensor([0, 15, 16, 31, 32, group // 2, group - 2, group - 1], device="cuda")
     check_attend(orc, cache, dtype, pool, table, q[:, at], n, d ** -0.5, 0, out[:, at], lse[:, at])
+
+
+def test_attend_empty_sequence_of_2_to_31_elements(apc):
+    """A sequence that holds nothing, its output of 2^31 elements: all of them are written."""
+    heads, group, d, page = 1 << 19, 16, 256, 16
+    say("attend 2^31 elements of an empty sequence")
+    k, v = (torch.empty((1, heads, page, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    c = apc.KvCache(k, v)
+    q = torch.empty((1, heads * group, d), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    table, lens = torch.zeros((1, 128), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    apc.apc_attend(c, q, table, lens, 0.1, out, apc.attend_workspace_tensor(c, 1, heads * group, 128), lse)
+    torch.cuda.synchronize()
+    assert not out.view(torch.int32).any() and torch.isneginf(lse).all()
