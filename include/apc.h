@@ -515,7 +515,7 @@ apc_status apc_attend_workspace(const apc_kv* c /* host */, int32_t b, int32_t q
  * written before).  No token left: o = 0, lse = -inf.  Nothing outside those
  * tokens reaches the result, whatever it holds.  Scores, the running maximum
  * and sum and the output's sums are float32; the weights of the values enter
- * the matrix product as two 16-bit parts each.
+ * the matrix product as two bf16 parts each (2^-16 of a weight, however light).
  * dt          type of q and out: the cache's, or APC_F16 / APC_BF16 where the
  *             cache is APC_E4M3.
  * q, out      sequence i's head a at i * row + a * head elements (strides

@@ -21,10 +21,15 @@
 //                  values of the same 8 keys; a lane owns DP / 16 consecutive
 //                  elements of those keys' rows, and pairs of keys are put
 //                  together in registers.  No value passes through LDS.
-// The weights enter as the sum of two 16-bit numbers (rounded, and the rounded
-// rest): one alone would lose 2^-9 (bf16) of every weight, two lose 2^-17, and
-// the matrix cores have time to spare.  e4m3 keys and values are converted
-// exactly to 16 bits; their scales join the scores and the weights in float32.
+// The weights enter as the sum of two bf16 (rounded, and the rounded rest): one
+// alone would lose 2^-8 of every weight, two lose 2^-16, of a weight however
+// light (two f16 would end at 2^-25 of the heaviest, and many light tokens make
+// the output where the heavy one's value is near 0).  f16 values are split into
+// two bf16 as well, exactly, so over f16 there are four products (16 sequences
+// of 1 to 1,000 tokens, 4 x 8 heads of 128: 16.0 us, 15.0 with f16 weights and
+// two products; 64 of 4,096 to 8,192, 12 heads of 64: 199 and 198).  e4m3 keys
+// and values are converted exactly to 16 bits; their scales join the scores and
+// the weights in float32.
 //
 // Bound by memory: every key and value is read once, into the registers that
 // the matrix instructions take.  A wave's next tile, of the same unit or of the
@@ -82,6 +87,15 @@ template <bool BF, bool HIGH> __device__ inline uint32_t from_e4m3(uint32_t w)
 {
     if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
+}
+
+// two f16 as the sum of two bf16 each: exact, 11 bits are 8 and 3
+__device__ inline void split_f16(uint32_t w, uint32_t& hi, uint32_t& lo)
+{
+    const f32x2 x = unpack<false>(w);
+    hi = pack<true>(x.x, x.y);
+    const f32x2 y = unpack<true>(hi);
+    lo = pack<true>(x.x - y.x, x.y - y.y);
 }
 
 // N dwords of keys or values.  ONCE: marked not to displace what is in the
@@ -170,7 +184,7 @@ template <int DT, int CDT, int DP, int NQ, int WAVES, bool CUT, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv c, AttendArgs a, AttendPlan p)
 {
     using T = typename Elem<DT>::T;
-    constexpr bool E8 = CDT == APC_E4M3, QBF = DT == APC_BF16, PBF = E8 || QBF;
+    constexpr bool E8 = CDT == APC_E4M3, QBF = DT == APC_BF16;
     constexpr int ES = E8 ? 1 : 2, EPL = DP / 16;               // values: elements of a row a lane owns
     constexpr int KW = 4 * ES, VW = EPL * ES / 4;               // dwords: 16 elements of a key, EPL of a value
     constexpr int SL = DP < 128 ? DP : 128;                     // elements of a round of the final sums
@@ -518,9 +532,9 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    hi[n][i] = pack<PBF>(w[2 * i], w[2 * i + 1]);
-                    const f32x2 y = unpack<PBF>(hi[n][i]);
-                    lo[n][i] = pack<PBF>(w[2 * i] - y.x, w[2 * i + 1] - y.y);
+                    hi[n][i] = pack<true>(w[2 * i], w[2 * i + 1]);
+                    const f32x2 y = unpack<true>(hi[n][i]);
+                    lo[n][i] = pack<true>(w[2 * i] - y.x, w[2 * i + 1] - y.y);
                 }
             }
 
@@ -534,22 +548,37 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                     const uint32_t y = vr[2 * i][w], z = vr[2 * i + 1][w];
                     if constexpr (E8) {
                         const uint32_t a01 = __builtin_amdgcn_perm(z, y, 0x05010400u), a23 = __builtin_amdgcn_perm(z, y, 0x07030602u);
-                        v[0][i] = from_e4m3<PBF, false>(a01);
-                        v[1][i] = from_e4m3<PBF, true>(a01);
-                        v[2][i] = from_e4m3<PBF, false>(a23);
-                        v[3][i] = from_e4m3<PBF, true>(a23);
+                        v[0][i] = from_e4m3<true, false>(a01);
+                        v[1][i] = from_e4m3<true, true>(a01);
+                        v[2][i] = from_e4m3<true, false>(a23);
+                        v[3][i] = from_e4m3<true, true>(a23);
                     } else {
                         v[0][i] = __builtin_amdgcn_perm(z, y, 0x05040100u);
                         v[1][i] = __builtin_amdgcn_perm(z, y, 0x07060302u);
                     }
                 }
 #pragma unroll
-                for (int n = 0; n < NQ; ++n)
+                for (int e = 0; e < PER; ++e) {
+                    u32x4 rest;
+                    if constexpr (CDT == APC_F16) {
 #pragma unroll
-                    for (int e = 0; e < PER; ++e) {
-                        o[n][w * PER + e] = mfma<PBF>(v[e], hi[n], o[n][w * PER + e]);
-                        o[n][w * PER + e] = mfma<PBF>(v[e], lo[n], o[n][w * PER + e]);
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t a, b;
+                            split_f16(v[e][i], a, b);
+                            v[e][i] = a, rest[i] = b;
+                        }
                     }
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) {
+                        f32x4& to = o[n][w * PER + e];
+                        to = mfma<true>(v[e], hi[n], to);
+                        to = mfma<true>(v[e], lo[n], to);
+                        if constexpr (CDT == APC_F16) {
+                            to = mfma<true>(rest, hi[n], to);
+                            to = mfma<true>(rest, lo[n], to);
+                        }
+                    }
+                }
             }
             if (inside || more) load_v(r);
             pc = inside ? pg : pn;

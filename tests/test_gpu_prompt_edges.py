@@ -1,9 +1,10 @@
 """Corners of the prompt model's operators against float64."""
+import numpy as np
 import pytest
 import torch
 
 from tests.gpu_check import say
-from tests.test_gpu_prompt_ops import KINDS, check_attend, make_attend, run_attend
+from tests.test_gpu_prompt_ops import KINDS, ROUND, TINY, TORCH, U, check_attend, f64, make_attend, run_attend
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +46,49 @@ def test_attend_empty_sequence_of_2_to_31_elements(apc):
     apc.apc_attend(c, q, table, lens, 0.1, out, apc.attend_workspace_tensor(c, 1, heads * group, 128), lse)
     torch.cuda.synchronize()
     assert not out.view(torch.int32).any() and torch.isneginf(lse).all()
+
+
+# ---- attention: chosen scores and values ------------------------------------------
+
+def one_sequence(cache, dtype, n, d, page=64):
+    """A pool with one sequence of n tokens, keys and values 0; setters of a token's row (exact in the cache's type)."""
+    mp = -(-n // page)
+    pool = [torch.zeros((mp, 1, page, d), device="cuda").to(TORCH[cache]) for _ in range(2)]
+    pool += [torch.ones((mp, 1, page), device="cuda") if cache == "e4m3" else None for _ in range(2)]
+    table = torch.arange(mp, dtype=torch.int32, device="cuda")[None].contiguous()
+    return pool, table, torch.tensor([n], dtype=torch.int32, device="cuda")
+
+
+def put(pool, j, row):
+    """row into token j of the pool's first sequence (pages in order)."""
+    page = pool.shape[2]
+    raw = row.to(pool.dtype)
+    if pool.element_size() == 1:
+        pool.view(torch.uint8)[j // page, 0, j % page] = raw.view(torch.uint8)
+    else:
+        pool[j // page, 0, j % page] = raw
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("below,value", [(15.0, 1.0), (17.4, 1.0), (17.4, 96.0), (22.0, 96.0), (25.0, 208.0)])
+def test_attend_light_weights_beside_a_heavy_one(apc, cache, dtype, below, value):
+    """One token takes nearly all the weight and has the value 0; the others' many small weights make the output."""
+    n, d, at = 32769, 64, 12345
+    say(f"attend light {dtype} over {cache} below={below} value={value}")
+    pool, table, lens = one_sequence(cache, dtype, n, d)
+    pool[1].copy_(torch.full(pool[1].shape, value, device="cuda"))
+    heavy = torch.zeros(d, device="cuda")
+    heavy[0] = below                                         # exact in every type (e4m3: 15, 17.4 -> 18, 22, 25 -> 24 or 26)
+    put(pool[0], at, heavy)
+    put(pool[1], at, torch.zeros(d, device="cuda"))
+    q = torch.zeros((1, 3, d), device="cuda").to(TORCH[dtype])
+    q[..., 0] = 1.0
+    out, lse = run_attend(apc, pool, table, q, lens, 1.0)
+    s = float(pool[0].float()[at // 64, 0, at % 64, 0])      # the heavy score as the cache holds it
+    rest = (n - 1) * np.exp(-s)
+    want = value * rest / (1 + rest)
+    # one score of one product, the others 0: the exponent's argument to 2 u s, the sums of n equal terms to n u at most
+    # and in blocks here (at most n / 128 + 64 additions on any path), weights to 2^-16
+    tol = want * (4 * U * s + 2 * (n / 128 + 64) * U + 2.0 ** -16 + ROUND[dtype] * 1.001) + TINY[dtype]
+    assert (np.abs(f64(out) - want) <= tol).all(), (f64(out).ravel()[0], want)
+    assert (np.abs(f64(lse) - (s + np.log1p(rest))) <= 2.0 ** -20 * s + 64 * U).all()
