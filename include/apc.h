@@ -512,10 +512,13 @@ apc_status apc_attend_workspace(const apc_kv* c /* host */, int32_t b, int32_t q
  * over the tokens j in [max(0, len - window), len) (window = 0: all), len =
  * lengths[i] cut to 0..max_pages * page, whose page entry is in 0..n_pages-1
  * (others are left out; the new token's own key and value are in the cache,
- * written before).  No token left: o = 0, lse = -inf.  Nothing outside those
- * tokens reaches the result, whatever it holds.  Scores, the running maximum
- * and sum and the output's sums are float32; the weights of the values enter
- * the matrix product as two bf16 parts each (2^-16 of a weight, however light).
+ * written before).  No token left, or none that scores above -inf: o = 0,
+ * lse = -inf.  Nothing outside those tokens reaches the result, whatever it
+ * holds; infinite and NaN values of theirs reach the elements that they stand
+ * in, as in a float32 sum (a call that meets them takes longer).  Scores, the
+ * running maximum and sum and the output's sums are float32; the weights of the
+ * values enter the matrix product as two bf16 parts each (2^-16 of a weight,
+ * however light).
  * dt          type of q and out: the cache's, or APC_F16 / APC_BF16 where the
  *             cache is APC_E4M3.
  * q, out      sequence i's head a at i * row + a * head elements (strides

@@ -44,9 +44,13 @@
 #include "convert.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace apc {
 namespace {
+
+// The kernel's parts are lambdas that hold its state in registers, so all of them have to be inlined.
+#define INLINE __attribute__((always_inline))
 
 constexpr int TILE = 32;
 constexpr int CUS = 256;
@@ -96,6 +100,20 @@ __device__ inline void split_f16(uint32_t w, uint32_t& hi, uint32_t& lo)
     hi = pack<true>(x.x, x.y);
     const f32x2 y = unpack<true>(hi);
     lo = pack<true>(x.x - y.x, x.y - y.y);
+}
+
+// the halves of w that hold infinities or NaN, as a mask
+template <bool BF> __device__ inline uint32_t not_finite(uint32_t w)
+{
+    constexpr uint32_t EXP = BF ? 0x7f80u : 0x7c00u;
+    return ((w & EXP) == EXP ? 0xffffu : 0u) | ((w >> 16 & EXP) == EXP ? 0xffff0000u : 0u);
+}
+
+// per half of w (bf16 weights): 1 for a weight, 0 for none, NaN for NaN, as f16 or bf16
+template <bool BF> __device__ inline uint32_t any_weight(uint32_t w)
+{
+    constexpr uint32_t ONE = BF ? 0x3f80u : 0x3c00u;
+    return ((w & 0xffffu) ? ONE : 0u) | ((w >> 16) ? ONE << 16 : 0u) | (not_finite<true>(w) & 0x7fff7fffu);
 }
 
 // N dwords of keys or values.  ONCE: marked not to displace what is in the
@@ -197,7 +215,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
     const int id = blockIdx.x, qt = id / 8 % p.qtiles, wg = id / 8 / p.qtiles * 8 + id % 8;
     if (wg >= p.groups) return;
     const int group = a.q_heads / c.heads, rows = group < NQ * 16 ? group : NQ * 16;
-    auto span_of = [&](int seq) { return Span(a, p, table_entry(a.lengths, seq)); };
+    auto span_of = [&](int seq) INLINE { return Span(a, p, table_entry(a.lengths, seq)); };
 
     Piece cur{0, 0, 0, 0, Span(a, p, 0)};                       // what is worked on
     int64_t unit_end = (int64_t)a.b * c.heads;                  // CUT: the stretch ends at this unit's tile off_end
@@ -218,7 +236,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         // The stretch, found by every wave for itself: a lane has four of every
         // 256 sequences, their costs (of one head) and the sum up to its last.
         struct Costs { int held[4], cost[4], upto, total; };
-        auto costs_of = [&](int seq0) {
+        auto costs_of = [&](int seq0) INLINE {
             Costs k;
             int sum = 0;
 #pragma unroll
@@ -300,7 +318,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         cur.n = cur.span.tiles;
     }
     // the piece after the unit's first u.off tiles, or of the next unit that the stretch reaches
-    auto settle = [&](Piece& u) {
+    auto settle = [&](Piece& u) INLINE {
         int64_t unit = (int64_t)u.seq * c.heads + u.head;
         while (u.off >= u.span.tiles && unit < unit_end) {
             u.off = 0;
@@ -320,7 +338,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
             return;
         }
     }
-    auto following = [&](const Piece& u) {
+    auto following = [&](Piece u) INLINE {
         Piece v = u;
         if constexpr (CUT) {
             v.off += u.n;
@@ -340,7 +358,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
 
     // queries: column col of tile n is query head (qt NQ + n) 16 + col of the group
     u32x4 q[NQ][DP / 32];
-    auto load_q = [&](const Piece& u) {
+    auto load_q = [&](Piece u) INLINE {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int qh = (qt * NQ + n) * 16 + col;
@@ -363,7 +381,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
     const int voff = 4 * g * row_bytes + (col * EPL < c.d ? col * EPL : 0) * ES;
 
     struct Pages { int32_t id[2]; };                            // of a tile's halves
-    auto find = [&](const Piece& u, int t) {
+    auto find = [&](Piece u, int t) INLINE {
         const int32_t* table = a.pages + u.seq * a.ld_pages;
         const int last = (u.span.len - 1) >> p.shift;
         Pages pg;
@@ -374,41 +392,233 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         }
         return pg;
     };
-    auto there = [&](int32_t page) { return (uint32_t)page < (uint64_t)c.n_pages; };
+    auto there = [&](int32_t page) INLINE { return (uint32_t)page < (uint64_t)c.n_pages; };
     struct Rows { int64_t at[2]; };                             // first rows of a tile's halves (of page 0 where there is none)
-    auto rows_of = [&](int head, int t, const Pages& pg) {
+    auto rows_of = [&](int head, int t, Pages pg) INLINE {
         Rows r;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             r.at[h] = (((int64_t)(there(pg.id[h]) ? pg.id[h] : 0) * c.heads + head) << p.shift) + ((t * TILE + 16 * h) & in_page);
         return r;
     };
-    uint32_t kr[2][DP / 64][KW], vr[8][VW];
-    f32x4 ks[2], vs[2];
-    auto load_k = [&](const Rows& r) {
+    struct Keys { uint32_t w[2][DP / 64][KW]; f32x4 scale[2]; };
+    struct Values { uint32_t w[8][VW]; f32x4 scale[2]; };
+    Keys key;
+    Values value;
+    auto load_k = [&](Keys& to, Rows r) INLINE {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint8_t* base = static_cast<const uint8_t*>(c.k) + r.at[h] * row_bytes;
 #pragma unroll
             for (int j = 0; j < DP / 64; ++j)
 #pragma unroll
-                for (int w = 0; w < KW; w += 4) stream<4, ONCE>(kr[h][j] + w, base + koff[j] + w * 4);
-            if constexpr (E8) ks[h] = *reinterpret_cast<const f32x4*>(c.k_scale + r.at[h] + 4 * g);
+                for (int w = 0; w < KW; w += 4) stream<4, ONCE>(to.w[h][j] + w, base + koff[j] + w * 4);
+            if constexpr (E8) to.scale[h] = *reinterpret_cast<const f32x4*>(c.k_scale + r.at[h] + 4 * g);
         }
     };
-    auto load_v = [&](const Rows& r) {
+    auto load_v = [&](Values& to, Rows r) INLINE {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint8_t* base = static_cast<const uint8_t*>(c.v) + r.at[h] * row_bytes;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int w = 0; w < VW; w += 4) stream<(VW < 4 ? VW : 4), ONCE>(vr[4 * h + i] + w, base + voff + i * row_bytes + w * 4);
-            if constexpr (E8) vs[h] = *reinterpret_cast<const f32x4*>(c.v_scale + r.at[h] + 4 * g);
+                for (int w = 0; w < VW; w += 4) stream<(VW < 4 ? VW : 4), ONCE>(to.w[4 * h + i] + w, base + voff + i * row_bytes + w * 4);
+            if constexpr (E8) to.scale[h] = *reinterpret_cast<const f32x4*>(c.v_scale + r.at[h] + 4 * g);
         }
     };
 
     const float to_log2 = a.scale * LOG2E;
+    constexpr int PER = 4 / ES;                                 // elements of a dword of values
+    // the i-th pair of keys' dwords put together, element by element
+    auto pairs = [](u32x4* v, int i, uint32_t y, uint32_t z) INLINE {
+        if constexpr (E8) {
+            const uint32_t a01 = __builtin_amdgcn_perm(z, y, 0x05010400u), a23 = __builtin_amdgcn_perm(z, y, 0x07030602u);
+            v[0][i] = from_e4m3<true, false>(a01);
+            v[1][i] = from_e4m3<true, true>(a01);
+            v[2][i] = from_e4m3<true, false>(a23);
+            v[3][i] = from_e4m3<true, true>(a23);
+        } else {
+            v[0][i] = __builtin_amdgcn_perm(z, y, 0x05040100u);
+            v[1][i] = __builtin_amdgcn_perm(z, y, 0x07060302u);
+        }
+    };
+    f32x4 o[NQ][EPL];
+    float m[NQ], l[NQ];
+    auto clear = [&]() INLINE {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            m[n] = LOWEST;
+            l[n] = 0.f;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) o[n][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    // The loaded tile t, its pages pg, into o, m and l; of what follows, where there
+    // is more, keys and values are loaded as soon as their registers are free.
+    // CAREFUL: right for infinite values, which a weight's second part (0, or
+    // negative) would make NaN, and near the end of float32's range, where weights
+    // must not pass 1.
+    auto add_tile = [&](auto care, Span span, int t, Pages pg, Keys& key, Values& value, bool more, Rows next) INLINE {
+        constexpr bool CAREFUL = decltype(care)::value;
+        // scores
+        f32x4 s[NQ][2];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                s[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < DP / 32; ++j) {
+                    u32x4 k;
+                    if constexpr (E8) {
+                        const uint32_t lo = key.w[h][j / 2][j % 2 * 2], hi = key.w[h][j / 2][j % 2 * 2 + 1];
+                        k = u32x4{from_e4m3<QBF, false>(lo), from_e4m3<QBF, true>(lo), from_e4m3<QBF, false>(hi),
+                                  from_e4m3<QBF, true>(hi)};
+                    } else {
+                        __builtin_memcpy(&k, &key.w[h][j / 2][j % 2 * 4], 16);
+                    }
+                    s[n][h] = mfma<QBF>(k, q[n][j], s[n][h]);
+                }
+            }
+        f32x4 factor[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            factor[h] = f32x4{to_log2, to_log2, to_log2, to_log2};
+            if constexpr (E8) factor[h] *= key.scale[h];
+        }
+        if (more) load_k(key, next);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) s[n][h] *= factor[h];
+
+        // the first and last tiles, and those with pages that are not there: their unseen keys drop out
+        const bool whole = t * TILE >= span.first && t * TILE + TILE <= span.len && there(pg.id[0]) && there(pg.id[1]);
+        if (!whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int tok = t * TILE + 16 * h + 4 * g + i;
+                    const bool seen = tok >= span.first && tok < span.len && there(pg.id[h]);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) s[n][h][i] = seen ? s[n][h][i] : -INFINITY;
+                    if constexpr (E8) value.scale[h][i] = seen ? value.scale[h][i] : 0.f;
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) value.w[4 * h + i][w] = seen ? value.w[4 * h + i][w] : 0u;
+                }
+        }
+
+        // the running maximum
+        float top[NQ];
+        bool over = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            top[n] = s[n][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top[n] = __builtin_fmaxf(top[n], s[n][i / 4][i % 4]);
+            over |= top[n] > m[n] + (CAREFUL ? 0.f : SLACK);
+        }
+        if (__any(over)) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                float y = __builtin_fmaxf(m[n], top[n]);
+                y = __builtin_fmaxf(y, __shfl_xor(y, 16, 64));
+                y = __builtin_fmaxf(y, __shfl_xor(y, 32, 64));
+                const float f = __builtin_amdgcn_exp2f(m[n] - y);
+                m[n] = y;
+                l[n] *= f;
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) o[n][e] *= f;
+            }
+        }
+
+        // weights, in two parts
+        u32x4 hi[NQ], lo[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(s[n][i / 4][i % 4] - m[n]);
+                l[n] += w[i];
+                if constexpr (E8) w[i] *= value.scale[i / 4][i % 4];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                hi[n][i] = pack<true>(w[2 * i], w[2 * i + 1]);
+                const f32x2 y = unpack<true>(hi[n][i]);
+                lo[n][i] = pack<true>(w[2 * i] - y.x, w[2 * i + 1] - y.y);
+            }
+        }
+
+        // infinite and NaN values, or e4m3 weights: their products alone, and 0 in their place after that
+        if constexpr (CAREFUL) {
+            u32x4 x[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (E8) {
+                        const uint32_t out = not_finite<true>(hi[n][i]);
+                        x[n][i] = hi[n][i] & out;
+                        hi[n][i] &= ~out;
+                        lo[n][i] &= ~out;
+                    } else {
+                        x[n][i] = any_weight<QBF>(hi[n][i]);
+                    }
+                }
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+                u32x4 v[PER];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t y = value.w[2 * i][w], z = value.w[2 * i + 1][w];
+                    if constexpr (!E8) {
+                        y &= not_finite<QBF>(y), z &= not_finite<QBF>(z);
+                        value.w[2 * i][w] ^= y, value.w[2 * i + 1][w] ^= z;
+                    }
+                    pairs(v, i, y, z);
+                }
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) o[n][w * PER + e] = mfma<E8 || QBF>(v[e], x[n], o[n][w * PER + e]);
+            }
+        }
+
+        // values: element e of every key's row, keys in pairs
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+            u32x4 v[PER];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pairs(v, i, value.w[2 * i][w], value.w[2 * i + 1][w]);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                u32x4 rest;
+                if constexpr (CDT == APC_F16) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t a, b;
+                        split_f16(v[e][i], a, b);
+                        v[e][i] = a, rest[i] = b;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    f32x4& to = o[n][w * PER + e];
+                    to = mfma<true>(v[e], hi[n], to);
+                    to = mfma<true>(v[e], lo[n], to);
+                    if constexpr (CDT == APC_F16) {
+                        to = mfma<true>(rest, hi[n], to);
+                        to = mfma<true>(rest, lo[n], to);
+                    }
+                }
+            }
+        }
+        if (more) load_v(value, next);
+    };
     int parts = 0;                                              // partial results written
     int turn = 0;
     int t = cur.begin() + wave;                                 // this wave's tile, loaded or on its way
@@ -416,8 +626,8 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
     if (t < cur.end()) {
         pc = find(cur, t);
         const Rows r = rows_of(cur.head, t, pc);
-        load_k(r);
-        load_v(r);
+        load_k(key, r);
+        load_v(value, r);
     }
     load_q(cur);
     while (true) {
@@ -430,160 +640,44 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         if (t + WAVES < end) pg = find(cur, t + WAVES);
         if (t >= end && more) {
             const Rows r = rows_of(nxt.head, t_nxt, pn);
-            load_k(r);
-            load_v(r);
+            load_k(key, r);
+            load_v(value, r);
         }
-        f32x4 o[NQ][EPL];
-        float m[NQ], l[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            m[n] = LOWEST;
-            l[n] = 0.f;
-#pragma unroll
-            for (int e = 0; e < EPL; ++e) o[n][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-
+        clear();
         while (t < end) {
             const bool inside = t + WAVES < end;
-            // scores
-            f32x4 s[NQ][2];
-#pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    s[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int j = 0; j < DP / 32; ++j) {
-                        u32x4 k;
-                        if constexpr (E8) {
-                            const uint32_t lo = kr[h][j / 2][j % 2 * 2], hi = kr[h][j / 2][j % 2 * 2 + 1];
-                            k = u32x4{from_e4m3<QBF, false>(lo), from_e4m3<QBF, true>(lo), from_e4m3<QBF, false>(hi),
-                                      from_e4m3<QBF, true>(hi)};
-                        } else {
-                            __builtin_memcpy(&k, &kr[h][j / 2][j % 2 * 4], 16);
-                        }
-                        s[n][h] = mfma<QBF>(k, q[n][j], s[n][h]);
-                    }
-                }
-            f32x4 factor[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                factor[h] = f32x4{to_log2, to_log2, to_log2, to_log2};
-                if constexpr (E8) factor[h] *= ks[h];
-            }
             const Rows r = inside ? rows_of(cur.head, t + WAVES, pg) : rows_of(nxt.head, t_nxt, pn);
-            if (inside || more) load_k(r);
-#pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) s[n][h] *= factor[h];
-
-            // the first and last tiles, and those with pages that are not there: their unseen keys drop out
-            const bool whole = t * TILE >= cur.span.first && t * TILE + TILE <= cur.span.len && there(pc.id[0]) && there(pc.id[1]);
-            if (!whole) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int tok = t * TILE + 16 * h + 4 * g + i;
-                        const bool seen = tok >= cur.span.first && tok < cur.span.len && there(pc.id[h]);
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n) s[n][h][i] = seen ? s[n][h][i] : -INFINITY;
-                        if constexpr (E8) vs[h][i] = seen ? vs[h][i] : 0.f;
-#pragma unroll
-                        for (int w = 0; w < VW; ++w) vr[4 * h + i][w] = seen ? vr[4 * h + i][w] : 0u;
-                    }
-            }
-
-            // the running maximum
-            float top[NQ];
-            bool over = false;
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                top[n] = s[n][0][0];
-#pragma unroll
-                for (int i = 1; i < 8; ++i) top[n] = __builtin_fmaxf(top[n], s[n][i / 4][i % 4]);
-                over |= top[n] > m[n] + SLACK;
-            }
-            if (__any(over)) {
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) {
-                    float y = __builtin_fmaxf(m[n], top[n]);
-                    y = __builtin_fmaxf(y, __shfl_xor(y, 16, 64));
-                    y = __builtin_fmaxf(y, __shfl_xor(y, 32, 64));
-                    const float f = __builtin_amdgcn_exp2f(m[n] - y);
-                    m[n] = y;
-                    l[n] *= f;
-#pragma unroll
-                    for (int e = 0; e < EPL; ++e) o[n][e] *= f;
-                }
-            }
-
-            // weights, in two parts
-            u32x4 hi[NQ], lo[NQ];
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                float w[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    w[i] = __builtin_amdgcn_exp2f(s[n][i / 4][i % 4] - m[n]);
-                    l[n] += w[i];
-                    if constexpr (E8) w[i] *= vs[i / 4][i % 4];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    hi[n][i] = pack<true>(w[2 * i], w[2 * i + 1]);
-                    const f32x2 y = unpack<true>(hi[n][i]);
-                    lo[n][i] = pack<true>(w[2 * i] - y.x, w[2 * i + 1] - y.y);
-                }
-            }
-
-            // values: element e of every key's row, keys in pairs
-#pragma unroll
-            for (int w = 0; w < VW; ++w) {
-                constexpr int PER = 4 / ES;
-                u32x4 v[PER];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t y = vr[2 * i][w], z = vr[2 * i + 1][w];
-                    if constexpr (E8) {
-                        const uint32_t a01 = __builtin_amdgcn_perm(z, y, 0x05010400u), a23 = __builtin_amdgcn_perm(z, y, 0x07030602u);
-                        v[0][i] = from_e4m3<true, false>(a01);
-                        v[1][i] = from_e4m3<true, true>(a01);
-                        v[2][i] = from_e4m3<true, false>(a23);
-                        v[3][i] = from_e4m3<true, true>(a23);
-                    } else {
-                        v[0][i] = __builtin_amdgcn_perm(z, y, 0x05040100u);
-                        v[1][i] = __builtin_amdgcn_perm(z, y, 0x07060302u);
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < PER; ++e) {
-                    u32x4 rest;
-                    if constexpr (CDT == APC_F16) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t a, b;
-                            split_f16(v[e][i], a, b);
-                            v[e][i] = a, rest[i] = b;
-                        }
-                    }
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) {
-                        f32x4& to = o[n][w * PER + e];
-                        to = mfma<true>(v[e], hi[n], to);
-                        to = mfma<true>(v[e], lo[n], to);
-                        if constexpr (CDT == APC_F16) {
-                            to = mfma<true>(rest, hi[n], to);
-                            to = mfma<true>(rest, lo[n], to);
-                        }
-                    }
-                }
-            }
-            if (inside || more) load_v(r);
+            add_tile(std::false_type{}, cur.span, t, pc, key, value, inside || more, r);
             pc = inside ? pg : pn;
             t += WAVES;
             if (t + WAVES < end) pg = find(cur, t + WAVES);
+        }
+        // Infinities or NaN came out: once more with care, one tile after the other,
+        // in registers of its own and the next tile loaded again after it, so that the
+        // loop above keeps the registers it has without this (as one loop of both: 64
+        // sequences of 4,096 to 8,192, 12 heads of 64, e4m3: 124 us, 118 so).
+        float z = 0.f;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int e = 0; e < EPL; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z = __builtin_fmaf(o[n][e][i], 0.f, z);
+        if (__builtin_expect(__any(z != 0.f), 0)) {
+            clear();
+            for (int again = cur.begin() + wave; again < end; again += WAVES) {
+                const Pages at = find(cur, again);
+                const Rows r = rows_of(cur.head, again, at);
+                Keys k;
+                Values v;
+                load_k(k, r);
+                load_v(v, r);
+                add_tile(std::true_type{}, cur.span, again, at, k, v, false, r);
+            }
+            // (where no tile follows, the first of the pool, which nobody reads)
+            const Rows r = rows_of(more ? nxt.head : 0, more ? t_nxt : 0, pn);
+            load_k(key, r);
+            load_v(value, r);
         }
         if (nxt.seq >= 0) load_q(nxt);
 
@@ -598,8 +692,8 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
             }
         }
         const bool whole_unit = cur.n == cur.span.tiles;
-        constexpr int TPH = 4 * WAVES, PER = SL / TPH;          // threads of a head, elements of a thread
-        const int hrow = threadIdx.x / TPH, dcol = threadIdx.x % TPH * PER;
+        constexpr int TPH = 4 * WAVES, OWN = SL / TPH;          // threads of a head, elements of a thread
+        const int hrow = threadIdx.x / TPH, dcol = threadIdx.x % TPH * OWN;
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -620,7 +714,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                 // where the compiler makes any here, would be lost in the threads that a branch leaves out
                 const int qh = (qt * NQ + n) * 16 + hrow;
                 const bool mine = qh < group && d0 + dcol < c.d;
-                float top = LOWEST, sum = 0.f, v[PER] = {};
+                float top = LOWEST, sum = 0.f, v[OWN] = {};
 #pragma unroll
                 for (int w = 0; w < WAVES; ++w) top = __builtin_fmaxf(top, ml[turn][w][n * 16 + hrow][0]);
 #pragma unroll
@@ -628,18 +722,18 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                     const float f = __builtin_amdgcn_exp2f(ml[turn][w][n * 16 + hrow][0] - top);
                     sum = __builtin_fmaf(f, ml[turn][w][n * 16 + hrow][1], sum);
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) v[i] = __builtin_fmaf(f, part[w][hrow][dcol + i], v[i]);
+                    for (int i = 0; i < OWN; ++i) v[i] = __builtin_fmaf(f, part[w][hrow][dcol + i], v[i]);
                 }
                 if (!CUT || whole_unit) {
                     const int64_t qrow = (int64_t)cur.head * group + qh;
                     const float f = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
+                    for (int i = 0; i < OWN; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
                     T* const to = static_cast<T*>(a.out) + cur.seq * a.out_row + qrow * a.out_head + d0 + dcol;
                     // d is a multiple of 16: a thread's elements, where they are more, can end past it
-                    constexpr int ST = PER < 16 ? PER : 16;
+                    constexpr int ST = OWN < 16 ? OWN : 16;
 #pragma unroll
-                    for (int i = 0; i < PER; i += ST)
+                    for (int i = 0; i < OWN; i += ST)
                         if (mine && d0 + dcol + i < c.d) store_values<DT, ST>(to + i, v + i);
                     if (a.lse && mine && d0 + dcol == 0)
                         a.lse[(int64_t)cur.seq * a.q_heads + qrow] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
@@ -647,7 +741,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                     const int64_t slot = (((int64_t)wg * p.qtiles + qt) * 2 + parts) * rows + n * 16 + hrow;
                     float* po = partial_sums(a, p) + slot * DP + d0 + dcol;
 #pragma unroll
-                    for (int i = 0; i < PER; i += 4) *reinterpret_cast<f32x4*>(po + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+                    for (int i = 0; i < OWN; i += 4) *reinterpret_cast<f32x4*>(po + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
                     if (d0 + dcol == 0) {
                         float* pm = partial_stats(a, p, rows, DP) + slot * 2;
                         pm[0] = top;

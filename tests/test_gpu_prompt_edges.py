@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests.gpu_check import say
-from tests.test_gpu_prompt_ops import KINDS, ROUND, TINY, TORCH, U, check_attend, f64, make_attend, run_attend
+from tests.test_gpu_prompt_ops import KINDS, ROUND, TINY, TORCH, U, check_attend, f64, make_attend, run_attend, stored
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +92,89 @@ def test_attend_light_weights_beside_a_heavy_one(apc, cache, dtype, below, value
     tol = want * (4 * U * s + 2 * (n / 128 + 64) * U + 2.0 ** -16 + ROUND[dtype] * 1.001) + TINY[dtype]
     assert (np.abs(f64(out) - want) <= tol).all(), (f64(out).ravel()[0], want)
     assert (np.abs(f64(lse) - (s + np.log1p(rest))) <= 2.0 ** -20 * s + 64 * U).all()
+
+
+def reference(q, k, v, scale):
+    """(out, lse, tol of out without the output's rounding) of one sequence and head, float64 rows k, v; tokens whose
+    score is -inf leave the sums (their weight is 0) but for infinite and NaN values, which 0 turns into NaN."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        s = scale * (k @ q)
+        w = np.exp(s - s.max())
+        out = (w[:, None] * v).sum(axis=0) / w.sum()
+        some = np.isfinite(s)
+        e = (k.shape[1] + 24) * U * (np.abs(scale) * (np.abs(k[some]) @ np.abs(q)).max())
+        spread = (w[some, None] * np.abs(v[some])).sum(axis=0) / w.sum()
+        return out, s.max() + np.log(w.sum()), spread * (4 * e + 2 * (len(s) + 64) * U + 2.0 ** -16), 2 * e + (len(s) + 64) * U
+
+
+def rows_of(orc, cache, pool, scale, table, n):
+    """float64 rows of the first n tokens of the only sequence, head 0."""
+    x = orc.kv_values(cache, stored(pool))
+    with np.errstate(invalid="ignore"):
+        if scale is not None:
+            x = x * scale.cpu().numpy().astype(np.float64)[..., None]
+    return np.concatenate([x[p, 0] for p in table[0].tolist()])[:n]
+
+
+def check_one(orc, cache, dtype, pool, table, q, n, scale, out, lse):
+    k, v = rows_of(orc, cache, pool[0], pool[2], table, n), rows_of(orc, cache, pool[1], pool[3], table, n)
+    got, gl = f64(out)[0], f64(lse)[0]
+    for h in range(q.shape[1]):
+        want, wl, tol, ltol = reference(f64(q)[0, h], k, v, scale)
+        some = np.isfinite(want)
+        assert np.array_equal(got[h][~some], want[~some], equal_nan=True), (got[h][~some], want[~some])
+        bad = ~(np.abs(got[h] - want)[some] <= (tol + np.abs(want) * ROUND[dtype] * 1.001 + TINY[dtype])[some])
+        assert not bad.any(), (np.abs(got[h] - want)[some][bad].max())
+        assert abs(gl[h] - wl) <= ltol + 2.0 ** -20 * abs(wl)
+
+
+LONG = [5, 70, 333, 5000]
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("group,d", [(1, 16), (3, 64), (5, 80), (4, 128), (20, 128), (2, 192), (18, 256)])
+def test_attend_infinite_values(apc, orc, cache, dtype, group, d):
+    """An infinite value of a token with weight makes its element infinite, two of different sign or a NaN make it NaN,
+    and the other elements are what they were."""
+    for n in LONG:
+        say(f"attend infinite values {dtype} over {cache} group={group} d={d} n={n}")
+        pool, table, q = make_attend(d + n, 1, 1, group, d, 16, -(-n // 16), cache, dtype)
+        lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+        at = lambda j: (table[0, j // 16].item(), 0, j % 16)
+        if cache == "e4m3":
+            code = pool[1].view(torch.uint8)
+            code[at(n - 1)][:6] = torch.tensor([0x7e, 0xfe, 0x00, 0x01, 0x81, 0x7f], dtype=torch.uint8, device="cuda")
+            pool[3][at(n - 1)] = float("inf")
+        else:
+            v = pool[1]
+            v[at(0)][1], v[at(n - 1)][2] = float("inf"), float("-inf")
+            v[at(n // 2)][3], v[at(1)][3] = float("inf"), float("inf")
+            v[at(n // 3)][4], v[at(n - 1)][4] = float("inf"), float("-inf")
+            v[at(n // 2)][5], v[at(n - 1)][d - 1] = float("nan"), float("inf")
+        scale = 0.02 if cache == "e4m3" else d ** -0.5       # no token's weight vanishes
+        pool[2] is None or pool[2].clamp_(max=0.3)
+        out, lse = run_attend(apc, pool, table, q, lens, scale)
+        check_one(orc, cache, dtype, pool, table, q, n, scale, out, lse)
+        again = run_attend(apc, pool, table, q, lens, scale)
+        assert torch.equal(out.view(torch.int16), again[0].view(torch.int16)) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("cache,dtype", [("bf16", "bf16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("n", [300, 9000])
+def test_attend_values_at_the_end_of_the_range(apc, orc, cache, dtype, n):
+    """Two tokens of values near float32's largest, the later one with the larger score: their mean is finite."""
+    say(f"attend large values {dtype} over {cache} n={n}")
+    d = 64
+    pool, table, lens = one_sequence(cache, dtype, n, d)
+    for j, score in ((0, 0.0), (256, 4.0)):
+        row = torch.zeros(d, device="cuda")
+        row[0], row[1] = score, 30.0
+        put(pool[0], j, row)
+        put(pool[1], j, torch.full((d,), 448.0 if cache == "e4m3" else 3.0e38, device="cuda"))
+        if cache == "e4m3":
+            pool[3][j // 64, 0, j % 64] = 6.7e35
+    q = torch.zeros((1, 2, d), device="cuda").to(TORCH[dtype])
+    q[..., 0], q[..., 1] = 1.0, 1.0
+    out, lse = run_attend(apc, pool, table, q, lens, 1.0)
+    assert torch.isfinite(out).all()
+    check_one(orc, cache, dtype, pool, table, q, n, 1.0, out, lse)
