@@ -372,12 +372,17 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         }
     };
 
-    // a lane's places in a row; past a row's end (d < DP) it reads another
-    // lane's elements: they meet zeros of q, or columns that are not stored
+    // a lane's places in a row; past a row's end (d < DP) it reads other elements
+    // of the row: of keys they meet zeros of q, and are zeroed where they can be
+    // infinite; of values they go into columns that are not stored
     const int row_bytes = c.d * ES, in_page = c.page - 1;
     int koff[DP / 64];
+    bool in_row[DP / 64];
 #pragma unroll
-    for (int j = 0; j < DP / 64; ++j) koff[j] = col * row_bytes + (j * 64 + g * 16 < c.d ? j * 64 + g * 16 : 0) * ES;
+    for (int j = 0; j < DP / 64; ++j) {
+        in_row[j] = j < DP / 128 || j * 64 + g * 16 < c.d;      // where DP is 128 or 256, d > DP / 2
+        koff[j] = col * row_bytes + (in_row[j] ? j * 64 + g * 16 : 0) * ES;
+    }
     const int voff = 4 * g * row_bytes + (col * EPL < c.d ? col * EPL : 0) * ES;
 
     struct Pages { int32_t id[2]; };                            // of a tile's halves
@@ -477,6 +482,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                                   from_e4m3<QBF, true>(hi)};
                     } else {
                         __builtin_memcpy(&k, &key.w[h][j / 2][j % 2 * 4], 16);
+                        if (j / 2 >= DP / 128) k = in_row[j / 2] ? k : u32x4{0, 0, 0, 0};
                     }
                     s[n][h] = mfma<QBF>(k, q[n][j], s[n][h]);
                 }

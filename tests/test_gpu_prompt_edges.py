@@ -159,6 +159,28 @@ def test_attend_infinite_values(apc, orc, cache, dtype, group, d):
         assert torch.equal(out.view(torch.int16), again[0].view(torch.int16)) and torch.equal(lse, again[1])
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("group,d", [(1, 16), (2, 48), (3, 64), (5, 80), (2, 96), (4, 128), (20, 112), (2, 144), (2, 192), (4, 256)])
+def test_attend_infinite_keys(apc, orc, dtype, group, d):
+    """A key that scores minus infinity has no weight, whatever its other elements and the head's size."""
+    for n in LONG:
+        say(f"attend infinite keys {dtype} group={group} d={d} n={n}")
+        pool, table, q = make_attend(d + n, 1, 1, group, d, 16, -(-n // 16), dtype, dtype)
+        lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+        at = lambda j: (table[0, j // 16].item(), 0, j % 16)
+        for e in (0, 7, d - 1):
+            q[..., e] = q[..., e].abs() + 0.25
+        for j, e in ((0, 0), (n - 2, 7), (n // 2, d - 1)):
+            pool[0][at(j)][e] = float("-inf")
+        pool[0][at(n // 2)][0] = float("-inf")
+        out, lse = run_attend(apc, pool, table, q, lens, d ** -0.5)
+        assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+        check_one(orc, dtype, dtype, pool, table, q, n, d ** -0.5, out, lse)
+        pool[0][table[0].long(), 0, :, 0] = float("-inf")     # no token scores above it
+        out, lse = run_attend(apc, pool, table, q, lens, d ** -0.5)
+        assert (out == 0).all() and torch.isneginf(lse).all()
+
+
 @pytest.mark.parametrize("cache,dtype", [("bf16", "bf16"), ("e4m3", "bf16")])
 @pytest.mark.parametrize("n", [300, 9000])
 def test_attend_values_at_the_end_of_the_range(apc, orc, cache, dtype, n):
