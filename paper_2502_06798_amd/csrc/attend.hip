@@ -356,22 +356,6 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         return v;
     };
 
-    // queries: column col of tile n is query head (qt NQ + n) 16 + col of the group
-    u32x4 q[NQ][DP / 32];
-    auto load_q = [&](Piece u) INLINE {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            const int qh = (qt * NQ + n) * 16 + col;
-            const T* row = static_cast<const T*>(a.q) + u.seq * a.q_row + (int64_t)(u.head * group + qh) * a.q_head;
-#pragma unroll
-            for (int j = 0; j < DP / 32; ++j) {
-                const int d = j / 2 * 64 + g * 16 + j % 2 * 8;
-                q[n][j] = u32x4{0, 0, 0, 0};
-                if (qh < group && d < c.d) __builtin_memcpy(&q[n][j], row + d, 16);
-            }
-        }
-    };
-
     // a lane's places in a row; past a row's end (d < DP) it reads other elements
     // of the row: of keys they meet zeros of q, and are zeroed where they can be
     // infinite; of values they go into columns that are not stored
@@ -384,6 +368,26 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         koff[j] = col * row_bytes + (in_row[j] ? j * 64 + g * 16 : 0) * ES;
     }
     const int voff = 4 * g * row_bytes + (col * EPL < c.d ? col * EPL : 0) * ES;
+
+    // Queries: column col of tile n is query head (qt NQ + n) 16 + col of the group,
+    // past its last head that one again, whose results nobody stores.  Loads that
+    // all lanes do, and zeros past a row's end put in when the loads are there.
+    u32x4 q[NQ][DP / 32];
+    auto load_q = [&](Piece u) INLINE {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int qh = (qt * NQ + n) * 16 + col, head = qh < group ? qh : group - 1;
+            const T* row = static_cast<const T*>(a.q) + u.seq * a.q_row + (int64_t)(u.head * group + head) * a.q_head;
+#pragma unroll
+            for (int j = 0; j < DP / 32; ++j) __builtin_memcpy(&q[n][j], row + (in_row[j / 2] ? j / 2 * 64 + g * 16 + j % 2 * 8 : 0), 16);
+        }
+    };
+    auto trim_q = [&]() INLINE {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int j = DP / 128 * 2; j < DP / 32; ++j) q[n][j] = in_row[j / 2] ? q[n][j] : u32x4{0, 0, 0, 0};
+    };
 
     struct Pages { int32_t id[2]; };                            // of a tile's halves
     auto find = [&](Piece u, int t) INLINE {
@@ -649,6 +653,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
             load_k(key, r);
             load_v(value, r);
         }
+        trim_q();
         clear();
         while (t < end) {
             const bool inside = t + WAVES < end;
@@ -718,6 +723,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
                 __syncthreads();
                 // every thread sums and only the stores are some threads': copies of the next round's registers,
                 // where the compiler makes any here, would be lost in the threads that a branch leaves out
+                // (the build looks for such copies)
                 const int qh = (qt * NQ + n) * 16 + hrow;
                 const bool mine = qh < group && d0 + dcol < c.d;
                 float top = LOWEST, sum = 0.f, v[OWN] = {};
