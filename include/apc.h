@@ -431,7 +431,7 @@ apc_status apc_merge_shards(const float* scores, const int32_t* idx, int32_t g, 
  * Root-mean-square norm of n rows of d elements, with the residual's addition
  * before it:
  *     h = x + res,   y = h / sqrt(mean(h^2) + eps) * weight,
- * in float32 throughout, each output rounded once (nearest-even).
+ * in float32 and this order throughout, each output rounded once (nearest-even).
  * dt          type of x, res, weight and sum: APC_F32, APC_F16 or APC_BF16.
  * out_dt      dt, or APC_E4M3: per row the scale s = amax / 448 of y and the
  *             codes of y / s, as apc_quantize_rows makes them.
@@ -445,7 +445,8 @@ apc_status apc_merge_shards(const float* scores, const int32_t* idx, int32_t g, 
  *             same rows.
  * out_scale   n float32 (APC_E4M3 only, else NULL).
  * eps         finite, >= 0.  A row whose float32 sum of squares overflows
- *             gives zeros; a zero row with eps = 0 gives NaN.
+ *             gives zeros; with eps = 0, one whose sum is 0 (a zero row, or
+ *             squares all below float32's range) is divided by 0.
  * 1 <= d <= APC_MAX_NORM_D.  n = 0 is a no-op.  Errors: APC_E_ARG,
  * APC_E_DTYPE.  Asynchronous on stream.
  */

@@ -2,13 +2,13 @@
 // rows' type or to e4m3 codes with a scale per row.
 //
 // T threads share a row and keep it in float32 registers, C chunks of 16 bytes
-// each, so the row and the residual are read once and everything after the
-// reduction comes from registers.  One reduction serves both passes: with
-// g = h w, y = g f has its largest magnitude where g has it (f > 0 is the
-// row's; rounding is monotonic), so the sum of squares and the largest |g| are
-// reduced together.  Bound by memory: each row's bytes once.  65,536 x 4,096
-// bf16 with residual to e4m3 309 us, 6.1 TB/s (a large copy reaches 4.6); short
-// rows to e4m3 by the arithmetic of a row's scale (994,131 x 112: 90 us, 3.8).
+// each, so the row and the residual are read once and everything after the first
+// reduction comes from registers.  y = (h f) w with the row's factor f, in this
+// order: h w alone can leave float32's range where y does not.  e4m3 rows need
+// the largest |y|, a second reduction.  Bound by memory: each row's bytes once.
+// 65,536 x 4,096 bf16 with residual to e4m3 311 us, 6.0 TB/s (a large copy
+// reaches 4.6); short rows to e4m3 by the arithmetic of a row's scale (994,131 x
+// 112: 90 us, 3.7).
 //
 // A row that does not end on a chunk ends with a chunk moved back to the row's
 // end: its first `skip` elements are another thread's too, left out of the sum
@@ -21,7 +21,7 @@ namespace apc {
 namespace {
 
 // Bytes of output from which it goes past the caches, where nobody would find
-// it again (65,536 x 1,024 bf16: 90 us, 93 without; 100,000 x 768 f16: 50 and 53).
+// it again (65,536 x 1,024 bf16 with residual: 91 us, 94 without; 100,000 x 768 f16: 50 and 53).
 constexpr int64_t PAST_CACHES = 64 << 20;
 constexpr int64_t MAX_GRID = 1 << 20;   // more rows than that many workgroups hold: a workgroup takes several
 
@@ -40,8 +40,10 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
     using E = typename Elem<DT>::T;
     using O = typename Elem<ODT>::T;
     constexpr int V = 16 / sizeof(E), ROWS = T > 256 ? 1 : 256 / T, WAVES = T / 64;
-    // up to three chunks a thread, the weight is loaded with the row and kept;
-    // longer rows read it twice from the cache, or they would spill registers
+    // up to three chunks a thread, the weight is loaded with the row; longer rows
+    // have no registers for it until the row is normed, and float32 rows beyond
+    // 16,384, with eight chunks, not for all of the residual either: they spill
+    // (4,096 x 32,768 with residual to e4m3: 715 us, 2.4 TB/s)
     constexpr bool KEEP_W = C <= 3;
     constexpr int CELLS = WAVES > 1 ? WAVES : 1;
     __shared__ float red_s[2][ROWS][CELLS];
@@ -67,7 +69,6 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
             }
         }
         float h[C][V], ss = 0.f;
-        uint32_t top = 0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float e[V];
@@ -82,9 +83,6 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
         for (int c = 0; c < C; ++c) {
             const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V, skip = at - from;
             if (at < a.d) {
-                float e[V];
-                if (ODT == APC_E4M3 && !KEEP_W && a.weight) rw[c].load(w + from);
-                if (ODT == APC_E4M3 && a.weight) rw[c].values(e);
                 if (a.d % V == 0) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) ss = __builtin_fmaf(h[c][i], h[c][i], ss);
@@ -92,57 +90,62 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_norm_rows(NormArgs a)
 #pragma unroll
                     for (int i = 0; i < V; ++i) ss = i < skip ? ss : __builtin_fmaf(h[c][i], h[c][i], ss);
                 }
-                if constexpr (ODT == APC_E4M3) {
-#pragma unroll
-                    for (int i = 0; i < V; i += 2) {
-                        const uint32_t m0 = magnitude(a.weight ? h[c][i] * e[i] : h[c][i]);
-                        const uint32_t m1 = magnitude(a.weight ? h[c][i + 1] * e[i + 1] : h[c][i + 1]);
-                        const uint32_t m = m0 > m1 ? m0 : m1;
-                        top = m > top ? m : top;
-                    }
-                }
             }
         }
+        // two sets of cells in turn: a wave may write the next row's while another
+        // still reads this row's
         ss = sum_over<(T < 64 ? T : 64)>(ss);
-        if constexpr (ODT == APC_E4M3) top = max_over<(T < 64 ? T : 64)>(top);
         if constexpr (WAVES > 1) {
-            // two sets of cells in turn: a wave may write the next row's while
-            // another still reads this row's
-            if ((threadIdx.x & 63) == 0) {
-                red_s[turn][own][t >> 6] = ss;
-                red_m[turn][own][t >> 6] = top;
-            }
+            if ((threadIdx.x & 63) == 0) red_s[turn][own][t >> 6] = ss;
             __syncthreads();
             ss = 0.f;
-            top = 0;
 #pragma unroll
-            for (int i = 0; i < WAVES; ++i) {
-                ss += red_s[turn][own][i];
-                top = red_m[turn][own][i] > top ? red_m[turn][own][i] : top;
-            }
+            for (int i = 0; i < WAVES; ++i) ss += red_s[turn][own][i];
         }
         const float f = rsqrt_of(__builtin_fmaf(ss, a.inv_d, a.eps));
-        // largest |y|; NaN where a g or the row's factor is NaN (0 * inf too)
-        const uint32_t ytop = top > 0x7f800000u ? top : magnitude(__uint_as_float(top) * f);
-        const RowCodes codes(ODT == APC_E4M3 ? ytop : 0u);
         E* sum = static_cast<E*>(a.sum) + (a.sum ? r * a.ld_sum : 0);
         O* out = static_cast<O*>(a.out) + r * a.ld_out;
+        uint32_t top = 0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V;
-            if (live && at < a.d) {
-                if (a.sum) store_values<DT, V>(sum + from, h[c], a.past);
-                float y[V];
+            if (at < a.d) {
+                if (live && a.sum) store_values<DT, V>(sum + from, h[c], a.past);
+                float e[V];
                 if (!KEEP_W && a.weight) rw[c].load(w + from);
-                if (a.weight) rw[c].values(y);
+                if (a.weight) rw[c].values(e);
 #pragma unroll
-                for (int i = 0; i < V; ++i) y[i] = (a.weight ? h[c][i] * y[i] : h[c][i]) * f;
-                if constexpr (ODT == APC_E4M3) codes.store<V>(out + from, y, a.past);
-                else store_values<ODT, V>(out + from, y, a.past);
+                for (int i = 0; i < V; ++i) h[c][i] = a.weight ? h[c][i] * f * e[i] : h[c][i] * f;
+                if constexpr (ODT == APC_E4M3) {
+#pragma unroll
+                    for (int i = 0; i < V; i += 2) {
+                        const uint32_t m0 = magnitude(h[c][i]), m1 = magnitude(h[c][i + 1]), m = m0 > m1 ? m0 : m1;
+                        top = m > top ? m : top;
+                    }
+                } else {
+                    if (live) store_values<ODT, V>(out + from, h[c], a.past);
+                }
             }
             if constexpr (C >= 4) __builtin_amdgcn_sched_barrier(0);   // chunk by chunk: interleaved, they spill
         }
-        if (ODT == APC_E4M3 && live && t == 0) a.out_scale[r] = codes.s;
+        if constexpr (ODT == APC_E4M3) {
+            top = max_over<(T < 64 ? T : 64)>(top);
+            if constexpr (WAVES > 1) {
+                if ((threadIdx.x & 63) == 0) red_m[turn][own][t >> 6] = top;
+                __syncthreads();
+                top = 0;
+#pragma unroll
+                for (int i = 0; i < WAVES; ++i) top = red_m[turn][own][i] > top ? red_m[turn][own][i] : top;
+            }
+            const RowCodes codes(top);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = (c * T + t) * V, from = at < a.d - V ? at : a.d - V;
+                if (live && at < a.d) codes.store<V, true>(out + from, h[c], a.past);
+                if constexpr (C >= 4) __builtin_amdgcn_sched_barrier(0);
+            }
+            if (live && t == 0) a.out_scale[r] = codes.s;
+        }
     }
 }
 
@@ -154,8 +157,7 @@ __global__ __launch_bounds__(256) void k_norm_short_rows(NormArgs a)
     using O = typename Elem<ODT>::T;
     constexpr int V = 16 / sizeof(E);
     for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.n; r += (int64_t)gridDim.x * 256) {
-        float h[V], g[V], ss = 0.f;
-        uint32_t top = 0;
+        float h[V], w[V], ss = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i < a.d) {
@@ -168,26 +170,27 @@ __global__ __launch_bounds__(256) void k_norm_short_rows(NormArgs a)
                     e.values(&v);
                     h[i] += v;
                 }
-                g[i] = h[i];
                 if (a.weight) {
-                    float v;
                     e.load(static_cast<const E*>(a.weight) + i);
-                    e.values(&v);
-                    g[i] *= v;
+                    e.values(&w[i]);
                 }
                 ss = __builtin_fmaf(h[i], h[i], ss);
-                const uint32_t m = magnitude(g[i]);
-                top = m > top ? m : top;
             }
         const float f = rsqrt_of(__builtin_fmaf(ss, a.inv_d, a.eps));
-        const RowCodes codes(top > 0x7f800000u ? top : magnitude(__uint_as_float(top) * f));
+        uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i < a.d) {
-                const float y = g[i] * f;
                 if (a.sum) store_values<DT, 1>(static_cast<E*>(a.sum) + r * a.ld_sum + i, &h[i]);
-                if constexpr (ODT == APC_E4M3) codes.store<1>(static_cast<O*>(a.out) + r * a.ld_out + i, &y);
-                else store_values<ODT, 1>(static_cast<O*>(a.out) + r * a.ld_out + i, &y);
+                h[i] = a.weight ? h[i] * f * w[i] : h[i] * f;
+                top = magnitude(h[i]) > top ? magnitude(h[i]) : top;
+            }
+        const RowCodes codes(top);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < a.d) {
+                if constexpr (ODT == APC_E4M3) codes.store<1>(static_cast<O*>(a.out) + r * a.ld_out + i, &h[i]);
+                else store_values<ODT, 1>(static_cast<O*>(a.out) + r * a.ld_out + i, &h[i]);
             }
         if (ODT == APC_E4M3) a.out_scale[r] = codes.s;
     }
@@ -204,8 +207,8 @@ void launch_t(const NormArgs& a, hipStream_t s)
 // Threads per row from the row's chunks alone, so that a row's bits do not
 // depend on the call's other rows: the fewest that leave two or three chunks to
 // each, and with them several loads in flight and few threads idle (100,000 x
-// 1,536 bf16 to e4m3: 64 threads with three 98 us, 128 with two 118; 65,536 x
-// 4,096 bf16 with residual to e4m3: 256 with two 309 us, 128 with four 323).
+// 1,536 bf16 to e4m3: 64 threads with three 86 us, 128 with two 99; 65,536 x
+// 4,096 bf16 with residual to e4m3: 256 with two 311 us, 128 with four 317).
 template <int DT, int ODT>
 hipError_t launch(const NormArgs& a, hipStream_t s)
 {

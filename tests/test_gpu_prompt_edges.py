@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests.gpu_check import say
-from tests.test_gpu_prompt_ops import KINDS, ROUND, TINY, TORCH, U, check_attend, f64, make_attend, run_attend, stored
+from tests.test_gpu_prompt_ops import KINDS, ROUND, TINY, TORCH, U, check_attend, check_norm, f64, gen, make_attend, run_attend, stored
 
 pytestmark = pytest.mark.gpu
 
@@ -200,3 +200,22 @@ def test_attend_values_at_the_end_of_the_range(apc, orc, cache, dtype, n):
     out, lse = run_attend(apc, pool, table, q, lens, 1.0)
     assert torch.isfinite(out).all()
     check_one(orc, cache, dtype, pool, table, q, n, 1.0, out, lse)
+
+
+# ---- norm ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("to8", [False, True])
+@pytest.mark.parametrize("size,weight", [(1e16, 1e25), (1e-15, 1e-30), (1e-18, 1e-25), (1e-8, 1e-33)])
+def test_norm_weights_far_from_one(apc, orc, dtype, to8, size, weight):
+    """h w leaves float32's range, or its normal part, where the normed row times w does not."""
+    for n, d in ((3, 3), (5, 48), (2, 999), (3, 4096), (2, 20000)):
+        say(f"norm extremes {dtype} to8={to8} n={n} d={d} size={size} weight={weight}")
+        g = gen(n + d)
+        x = (torch.randn((n, d), device="cuda", generator=g) * size).to(TORCH[dtype])
+        w = ((1 + torch.rand(d, device="cuda", generator=g)) * weight).to(TORCH[dtype])
+        out = torch.zeros((n, d), device="cuda").to(TORCH["e4m3" if to8 else dtype])
+        scale = torch.zeros(n, device="cuda") if to8 else None
+        apc.apc_norm_rows(x, out, w, None, None, scale, 0.0)
+        torch.cuda.synchronize()
+        check_norm(orc, x, None, w, out, scale, None, 0.0, dtype)
