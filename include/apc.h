@@ -464,7 +464,7 @@ apc_status apc_norm_rows(apc_dtype dt, apc_dtype out_dt, int64_t n, int32_t d, c
  */
 typedef struct {
     apc_dtype dt;        /* APC_F16, APC_BF16 or APC_E4M3 */
-    int32_t heads;       /* key-value heads, >= 1 */
+    int32_t heads;       /* key-value heads, 1 .. APC_MAX_ATTEND_ROWS */
     int32_t d;           /* elements per head: a multiple of 16, <= APC_MAX_HEAD_DIM */
     int32_t page;        /* tokens per page: a power of two, 16 <= page <= APC_MAX_PAGE */
     int64_t n_pages;     /* n_pages * page < 2^31 */

@@ -102,9 +102,10 @@ apc_status check_kv(const char* who, const apc_kv* c)
     if (!c) return fail(APC_E_ARG, "%s: NULL cache", who);
     if (c->dt != APC_F16 && c->dt != APC_BF16 && c->dt != APC_E4M3)
         return fail(APC_E_DTYPE, "%s: a key-value cache is f16, bf16 or e4m3 (got %d)", who, (int)c->dt);
-    if (c->heads < 1 || c->d < 16 || c->d > APC_MAX_HEAD_DIM || c->d % 16 != 0)
-        return fail(APC_E_ARG, "%s: need heads >= 1 and d a multiple of 16 up to %d (heads=%d d=%d)", who,
-                    APC_MAX_HEAD_DIM, c->heads, c->d);
+    // (the kernels count a token's rows, two a head, in 32 bits)
+    if (c->heads < 1 || c->heads > APC_MAX_ATTEND_ROWS || c->d < 16 || c->d > APC_MAX_HEAD_DIM || c->d % 16 != 0)
+        return fail(APC_E_ARG, "%s: need 1 <= heads <= %d and d a multiple of 16 up to %d (heads=%d d=%d)", who,
+                    APC_MAX_ATTEND_ROWS, APC_MAX_HEAD_DIM, c->heads, c->d);
     if (c->page < 16 || c->page > APC_MAX_PAGE || (c->page & (c->page - 1)) != 0)
         return fail(APC_E_ARG, "%s: page must be a power of two from 16 to %d (page=%d)", who, APC_MAX_PAGE, c->page);
     if (c->n_pages < 0 || c->n_pages > INT32_MAX / c->page)
