@@ -482,8 +482,9 @@ typedef struct {
  * k, v        t x heads x d: token i's head h at i * tok + h * head elements
  *             (strides k_tok, k_head, v_tok, v_head >= 0; d elements contiguous).
  * slots       t int32 (device): the slot of each token; a value outside the
- *             cache's slots (-1 for padding) writes nothing.  Two tokens with
- *             one slot leave either's rows there.
+ *             cache's slots (-1 for padding) writes nothing.  No slot inside may
+ *             stand twice: its rows would hold anything afterwards, parts of
+ *             both tokens' and one's codes with the other's scale among it.
  * t = 0 is a no-op.  Errors: APC_E_ARG, APC_E_DTYPE.  Asynchronous on stream.
  */
 apc_status apc_kv_write(const apc_kv* c /* host */, apc_dtype dt, int64_t t, const void* k, int64_t k_tok,

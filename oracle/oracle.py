@@ -565,7 +565,7 @@ def norm_rows(x, res, weight, eps: float):
 
 def kv_write(dtype: str, pool: np.ndarray, scale, x: np.ndarray, slots):
     """Writes rows x (t x heads x d float32) into pool (n_pages x heads x page x d, stored elements) and scale in
-    place; later tokens win where two share a slot."""
+    place (slots inside the pool are distinct)."""
     n_pages, heads, page, _ = pool.shape
     for i, s in enumerate(np.asarray(slots, dtype=np.int64)):
         if s < 0 or s >= n_pages * page:

@@ -458,7 +458,8 @@ def _kv_rows(c: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
 
 
 def apc_kv_write(c: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
-    """Keys and values (t x heads x d, tokens and heads strided as they come) into the cache's slots."""
+    """Keys and values (t x heads x d, tokens and heads strided as they come) into the cache's slots: each slot once,
+    or outside the cache (-1), where nothing is written."""
     dt, t, kp, kt, kh, vp, vt, vh, sp = _kv_rows(c, k, v, slots)
     rc = load().apc_kv_write(c.ref, dt, t, kp, kt, kh, vp, vt, vh, sp, _stream(stream))
     if rc:
