@@ -117,11 +117,11 @@ template <bool BF> __device__ inline uint32_t any_weight(uint32_t w)
 }
 
 // N dwords of keys or values.  ONCE: marked not to displace what is in the
-// caches (256 sequences of 100 to 2,048 tokens, bf16: 190 us, 212 without; 64 of
-// 16,384 to 32,768, e4m3: 530 and 570).  Not so where the next call may find them
-// there (16 of 1,024, bf16: 15.6 us, 21.1 marked), and where several workgroups
+// caches (256 sequences of 100 to 2,048 tokens, bf16: 191 us, 213 without; 64 of
+// 16,384 to 32,768, e4m3: 538 and 573).  Not so where the next call may find them
+// there (16 of 1,024, bf16: 15.9 us, 21.2 marked), and where several workgroups
 // have the query heads of one key-value head, the second of which finds what the
-// first read (64 sequences, 128 query heads on one of 128, bf16: 161 us, 234 marked).
+// first read (64 sequences, 128 query heads on one of 128, bf16: 160 us, 222 marked).
 template <int N, bool ONCE> __device__ inline void stream(uint32_t* to, const uint8_t* from)
 {
     if constexpr (N == 1) {
@@ -874,19 +874,19 @@ constexpr int SNAP = 16;                // in a stretch, units of up to so many 
 // Up to WIDE_UNITS units, a unit has a workgroup of eight waves, if it has one
 // to itself at all.  It has where even the table's longest would be no more
 // than WHOLE_UNIT bytes, which spares a second launch (64 x 8 units of 1,024
-// tokens, e4m3, heads of 128, 279 KB: 26.5 us, 32.1 in stretches; 4 x 8 of
-// 1,024, bf16, 524 KB: 19.9 and 15.9), or WHOLE_UNIT_MANY where there is a unit
-// for every other CU (32 x 8 of 1,024, bf16: 25.1 us, 31.1 in stretches; 16 x
-// 8: 21.1 and 21.3).
+// tokens, e4m3, heads of 128, 279 KB: 27.4 us, 32.9 in stretches; 4 x 8 of
+// 1,024, bf16, 524 KB: 15.5 either way; of 2,048: 24.5 and 17.0), or WHOLE_UNIT_MANY where there is a unit
+// for every other CU (32 x 8 of 1,024, bf16: 25.3 us, 31.8 in stretches; 16 x
+// 8: 16.0 and 20.5).
 constexpr int64_t WIDE_UNITS = 256;
 constexpr int64_t WHOLE_UNIT = 288 << 10, WHOLE_UNIT_MANY = 560 << 10;
 constexpr int MIN_SHARE = 8;            // tiles of a stretch, at least
 // Stretches: the workgroups that the chip holds at once.  Two a CU (64 long
-// sequences over e4m3: 530 us; one 624, three 550, four 535); four with rows of
+// sequences over e4m3: 538 us; one 627, three 558, four 543); four with rows of
 // 64 bytes, whose tiles are small (64 sequences of 8,192 to 16,384 tokens, 12
-// heads of 64, e4m3: 220 us, 230 with two); one with wide heads, which leave
-// registers for one (32 sequences of 4,096 to 8,192, 4 heads of 256, bf16: 148
-// us, 160 with two).
+// heads of 64, e4m3: 228 us, 235 with two); one with wide heads, which leave
+// registers for one (32 sequences of 4,096 to 8,192, 4 heads of 256, bf16: 149
+// us, 161 with two).
 int stretches(const apc_kv& c, int qtiles)
 {
     const int groups = padded(c.d) > 128 ? 256 : c.d * elem_bytes(c.dt) <= 64 ? 1024 : 512;
@@ -894,20 +894,20 @@ int stretches(const apc_kv& c, int qtiles)
 }
 // One wave has a unit to itself, and nothing to join, where the unit is a tile,
 // or where there are enough short units for every SIMD: of eight tiles at most
-// (256 x 8 units of 128 tokens, bf16, heads of 128: 25.7 us, 28.7 with four
-// waves; 149 x 11 of one to three, e4m3: 9.7 and 15.3), or of 32 with wide heads,
+// (256 x 8 units of 128 tokens, bf16, heads of 128: 25.5 us, 30.8 with four
+// waves; 149 x 11 of one to three, e4m3: 9.1 and 16.9), or of 32 with wide heads,
 // whose registers leave a CU a single workgroup of four (256 x 8 of 512, heads of
-// 256, e4m3: 99.8 us and 123.4; bf16, 1 MB a unit: 182 us, 206 in stretches).
+// 256, e4m3: 102.5 us and 125.7; bf16, 1 MB a unit: 183 us, 209 in stretches).
 // Narrower heads have no gain there, and lose where the lengths differ (256 x 12
-// of 1 to 500 tokens, heads of 64: 43.4 us and 40.2).
+// of 1 to 500 tokens, heads of 64: 47.2 us and 40.6).
 bool one_wave(int d, int64_t units, int64_t seen)
 {
     return seen <= 1 || (units >= 1024 && seen <= 8) || (padded(d) > 128 && units >= 2048 && seen <= 32);
 }
 // Calls that could read as much find little of it again in the 256 MB
 // last-level cache, even where a next call reads the same keys and values
-// (three caches in turn, 24 x 8 units of 1,024 tokens over bf16, 101 MB: 20.8 us,
-// 22.3 marked; 32 x 8, 134 MB: 26.9 and 25.0).
+// (three caches in turn, 24 x 8 units of 1,024 tokens over bf16, 101 MB: 21.1 us,
+// 22.7 marked; 32 x 8, 134 MB: 27.0 and 25.2).
 constexpr int64_t ONCE_BYTES = 100 << 20;
 constexpr int64_t UNCUT_GROUPS = 1 << 16;
 int64_t tiles_of(const apc_kv& c, int64_t max_pages) { return (max_pages * c.page + TILE - 1) / TILE; }
@@ -958,8 +958,8 @@ hipError_t launch_q(const apc_kv& c, const AttendArgs& a, const AttendPlan& p, h
     const int64_t units = (int64_t)a.b * c.heads;
     const bool by_unit = units <= p.groups;
     const dim3 joins((unsigned)((by_unit ? (int)units : p.groups) * p.qtiles), (unsigned)rows);
-    // few units are cut into many parts: more threads to read them (64 parts of
-    // 64 heads: 5.6 us, 7.3 with 256; 2,048 workgroups: 7.5 us, 4.9 with 256)
+    // few units are cut into many parts: more threads to read them (256 parts
+    // of 64 heads: 9.6 us, 14.7 with 256; 2,048 workgroups: 7.9 us, 5.9 with 256)
     if (joins.x * joins.y <= 512) k_attend_join<DT, DP, 512><<<joins, dim3(512), 0, s>>>(c, a, p, rows, by_unit);
     else k_attend_join<DT, DP, 256><<<joins, dim3(256), 0, s>>>(c, a, p, rows, by_unit);
     return hipGetLastError();

@@ -13,7 +13,7 @@
 // A row that does not end on a chunk ends with a chunk moved back to the row's
 // end: its first `skip` elements are another thread's too, left out of the sum
 // and stored by both with the same bits.  Every load of a row comes before the
-// reduction and every store after it, so that outputs may be the inputs' rows.
+// first reduction and every store after it, so that outputs may be the inputs' rows.
 #include "apc_internal.h"
 #include "convert.h"
 
