@@ -25,8 +25,8 @@ COUNTED = ["qs_f16.hip", "qs_bf16.hip", "qs_e4m3.hip", "qs8_f16.hip", "qs8_bf16.
 # outstanding as it knows to be newer than what it needs: operations that the
 # compiler adds only make a wait longer.  Its tiles of 256 queries spill a few
 # registers (bytes per lane, the other tiles none); more would cost time.  The
-# attention kernels use none.
-SCRATCH = {"tile_f32.hip": 0, "tile_f16.hip": 24, "tile_bf16.hip": 24, "tile_e4m3.hip": 12, "attend.hip": 0}
+# attention kernels use none, the norm's those of float32 rows beyond 16,384.
+SCRATCH = {"tile_f32.hip": 0, "tile_f16.hip": 24, "tile_bf16.hip": 24, "tile_e4m3.hip": 12, "attend.hip": 0, "norm.hip": 240}
 
 # Kernels in these sources keep values of every lane in registers across
 # branches that only some lanes take.  Where registers are short the compiler
