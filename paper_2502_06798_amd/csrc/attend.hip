@@ -40,8 +40,7 @@
 // us and 5.5 in the join (its workgroups end from 31 to 49 us: a CU's older
 // waves go first).  A call of little work is its latency: some 2 us to launch,
 // 2 for its share, 2 to 3 for its first keys, 2 for each further tile of a wave.
-#include "apc_internal.h"
-#include "convert.h"
+#include "attend_common.h"
 
 #include <cmath>
 #include <type_traits>
@@ -49,19 +48,9 @@
 namespace apc {
 namespace {
 
-// The kernel's parts are lambdas that hold its state in registers, so all of them have to be inlined.
-#define INLINE __attribute__((always_inline))
-
 constexpr int TILE = 32;
 constexpr int CUS = 256;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float LOWEST = -3.0e38f;      // below every score; finite, so that exp2(-inf - m) is 0
 constexpr float SLACK = 8.f;            // weights stay below 2^8
-
-using f32x4 = float __attribute__((ext_vector_type(4)));
-using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
-using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
-using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 
 // 16 x 16 x 32: D = A B + C; a lane's 8 values of A are row lane % 16, of B
 // column lane % 16, both at k = 8 (lane / 16); of D column lane % 16, rows 4 (lane / 16) + r
@@ -73,26 +62,6 @@ template <bool BF> __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-template <bool BF> __device__ inline uint32_t pack(float a, float b)
-{
-    const f32x2 x = {a, b};
-    if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
-}
-
-template <bool BF> __device__ inline f32x2 unpack(uint32_t w)
-{
-    if constexpr (BF) return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
-    else return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2);
-}
-
-// two e4m3 codes (the low or the high half of w) in 16 bits: exact
-template <bool BF, bool HIGH> __device__ inline uint32_t from_e4m3(uint32_t w)
-{
-    if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
-    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
-}
-
 // two f16 as the sum of two bf16 each: exact, 11 bits are 8 and 3
 __device__ inline void split_f16(uint32_t w, uint32_t& hi, uint32_t& lo)
 {
@@ -100,13 +69,6 @@ __device__ inline void split_f16(uint32_t w, uint32_t& hi, uint32_t& lo)
     hi = pack<true>(x.x, x.y);
     const f32x2 y = unpack<true>(hi);
     lo = pack<true>(x.x - y.x, x.y - y.y);
-}
-
-// the halves of w that hold infinities or NaN, as a mask
-template <bool BF> __device__ inline uint32_t not_finite(uint32_t w)
-{
-    constexpr uint32_t EXP = BF ? 0x7f80u : 0x7c00u;
-    return ((w & EXP) == EXP ? 0xffffu : 0u) | ((w >> 16 & EXP) == EXP ? 0xffff0000u : 0u);
 }
 
 // per half of w (bf16 weights): 1 for a weight, 0 for none, NaN for NaN, as f16 or bf16
@@ -133,15 +95,6 @@ template <int N, bool ONCE> __device__ inline void stream(uint32_t* to, const ui
         const V x = ONCE ? __builtin_nontemporal_load(p) : *p;
         __builtin_memcpy(to, &x, 4 * N);
     }
-}
-
-// An entry of an input table at an index that all lanes share.  The tables do
-// not change while the kernel runs, which the compiler cannot know; as constant
-// memory they are read with scalar loads, and what follows from them stays in
-// scalar registers.
-__device__ inline int32_t table_entry(const int32_t* table, int64_t i)
-{
-    return ((const __attribute__((address_space(4))) int32_t*)table)[i];
 }
 
 // a value that every lane holds alike, in scalar registers
