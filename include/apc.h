@@ -72,7 +72,8 @@ typedef enum {
 #define APC_MAX_PAGE 1024     /* most tokens of a key-value page */
 #define APC_MAX_TOKENS (1 << 30)       /* most tokens of one sequence's page table */
 #define APC_MAX_TABLE_TOKENS (1ll << 35)  /* most tokens of all page tables of one apc_attend, 256 added for each */
-#define APC_MAX_ATTEND_ROWS (1 << 23)  /* most sequences x query heads of one apc_attend */
+#define APC_MAX_ATTEND_ROWS (1 << 23)  /* most sequences x query heads of one apc_attend or apc_attend_prompt */
+#define APC_MAX_PROMPT_ROWS (1 << 29)  /* most new tokens x query heads of one apc_attend_prompt */
 
 /* opaque, immutable after build */
 typedef struct apc_cache apc_cache;
@@ -418,10 +419,11 @@ apc_status apc_merge_shards(const float* scores, const int32_t* idx, int32_t g, 
 /*
  * Operators of the prompt model (not a step of the paper, which takes prompt
  * embeddings as given: what a dispatcher that also runs the text model needs
- * to make them, one new token of every prompt at a time).  Rows of the new
- * tokens are normed (apc_norm_rows), their keys and values go into a paged
- * cache (apc_kv_write), attention reads it (apc_attend), and the last norm
- * leaves e4m3 rows with their scales, the form in which apc_match_batch takes
+ * to make them, from whole prompts at once or one new token of every prompt at a
+ * time).  Rows of the new tokens are normed (apc_norm_rows), queries and keys
+ * turned by their positions (apc_rotate), keys and values go into a paged
+ * cache (apc_kv_write), attention reads it (apc_attend_prompt, or apc_attend for
+ * one token of each sequence), and the last norm leaves e4m3 rows with their scales, the form in which apc_match_batch takes
  * queries.  These calls take strides in elements, so that views of wider rows
  * (a fused product's output) need no copy; their buffers need only the
  * alignment of their element type, except where 16 bytes are asked for.
@@ -541,6 +543,117 @@ apc_status apc_attend(const apc_kv* c /* host */, apc_dtype dt, const void* q, i
                       int32_t b, int32_t q_heads, const int32_t* pages, int32_t max_pages, int64_t ld_pages,
                       const int32_t* lengths, int32_t window, float scale, void* out, int64_t out_row,
                       int64_t out_head, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rotary positions: a description passed by address (host).  Of a head's d
+ * elements the first `rot` are turned in rot / 2 pairs, pair i by the angle
+ * position * freq[i].
+ */
+typedef struct {
+    int32_t rot;          /* even, 2 <= rot <= d */
+    int32_t interleaved;  /* 0: pair i is elements i and i + rot / 2; 1: 2 i and 2 i + 1 */
+    float mag;            /* factor of the turned elements, finite (1, or what a longer context asks for) */
+    const double* freq;   /* device, 8-byte aligned, rot / 2: angle of one position, in radians */
+} apc_rotary;
+
+/*
+ * Frequencies of rotary positions (host only):
+ *     f_i = base^(-2 i / rot),   n_i = original * f_i / (2 pi),
+ *     freq[i] = g f_i + (1 - g) f_i / factor,  g = (n_i - low) / (high - low) cut to 0..1.
+ * A context made `factor` times longer than the `original` positions that the
+ * model was trained on: what turns `high` times or more in them stays as it is,
+ * what turns `low` times or less is stretched.  original = 0: everything is
+ * (g = 0; low and high are not looked at); factor = 1: nothing.
+ * rot even, 2 <= rot <= APC_MAX_HEAD_DIM; base > 0, factor > 0, original >= 0,
+ * high > low (where original > 0), all finite.
+ * Errors: APC_E_ARG.
+ */
+apc_status apc_rotary_freqs(int32_t rot, double base, double factor, double original, double low, double high,
+                            double* freq /* host, rot / 2 */);
+
+/*
+ * Turns t x heads rows of d elements by their tokens' positions: of each pair
+ *     y_a = mag * (x_a cos w - x_b sin w),   y_b = mag * (x_b cos w + x_a sin w),
+ * w = positions[token] * freq[pair] in float64 and reduced there, the rest in
+ * float32 and rounded once (nearest-even).  Elements from rot on are copied.
+ * Queries and keys that stand side by side in a fused product's output are the
+ * heads of one call.  Frequencies of opposite sign turn back (and are the
+ * gradient's turn).
+ * dt          type of x and out: APC_F32, APC_F16 or APC_BF16.
+ * x, out      token i's head h at i * tok + h * head elements (strides x_tok,
+ *             x_head, out_tok, out_head >= 0; d elements contiguous).  out may be
+ *             x's own rows (same address and strides); else they must not
+ *             overlap, and no two rows of out may.
+ * positions   t int32 (device); a token whose position is negative (padding)
+ *             is left out: its rows of out stay as they were.
+ * 1 <= d <= APC_MAX_HEAD_DIM, heads >= 1, t * heads < 2^31.  t = 0 is a no-op.
+ * Errors: APC_E_ARG, APC_E_DTYPE.  Asynchronous on stream.
+ */
+apc_status apc_rotate(const apc_rotary* r /* host */, apc_dtype dt, int64_t t, int32_t heads, int32_t d, const void* x,
+                      int64_t x_tok, int64_t x_head, const int32_t* positions, void* out, int64_t out_tok,
+                      int64_t out_head, void* stream);
+
+/* Workspace bytes apc_attend_prompt needs for t new tokens of b sequences, q_heads
+   query heads and page tables of max_pages entries.  Never falls as t, b or
+   max_pages grows. */
+apc_status apc_attend_prompt_workspace(const apc_kv* c /* host */, int64_t t, int32_t b, int32_t q_heads,
+                                       int32_t max_pages, size_t* bytes /* host */);
+
+/*
+ * Attention of several new tokens of each of b sequences over the sequence's
+ * cached tokens, the new ones' keys and values among them (written before):
+ * whole prompts, the next piece of them, or single tokens.  The new tokens' rows
+ * stand one sequence after the other, sequence i's from starts[i] to
+ * starts[i + 1]; they are its last ones, so that the row starts[i] + r is the
+ * token at position p = len - (starts[i + 1] - starts[i]) + r, len = lengths[i]
+ * cut to 0..max_pages * page.  For query head a and its key-value head
+ * h = a / (q_heads / heads):
+ *     s_j = scale * <q, k_j>,  with a cap: cap * tanh(s_j / cap),
+ *     with slopes: less slopes[a] * |p - j|,
+ *     o = sum_j exp(s_j) v_j / sum_j exp(s_j),   lse = ln sum_j exp(s_j),
+ * over the tokens j < len that p sees: those up to itself, j <= p, and the
+ * sequence's first prefix[i], j < prefix[i] (prefix >= len: every token sees all);
+ * with a window of them those with |p - j| < window; and of these those whose
+ * page entry is in 0..n_pages-1.  Sequences do not see each other: documents
+ * packed into one call are sequences of it.  A row that sees no token, or none
+ * that scores above -inf: o = 0, lse = -inf (a sequence with more new tokens than
+ * len has rows at negative positions, which see its prefix at most).  Nothing
+ * outside the tokens that a row sees reaches its result, whatever it holds;
+ * infinite and NaN values of theirs leave the elements that they stand in
+ * infinite or NaN (a call that meets them, or values near the end of float32's
+ * range, takes longer).
+ * Scores, the running maximum and sum and the output's sums are float32.  The
+ * weights of the values enter the matrix product rounded to the type of q (an
+ * error of half a step of each weight), or, for f16 over an e4m3 cache and where
+ * sequences have few new tokens, in two parts (2^-16 of a weight); over f16
+ * caches a weight below 2^-25 of its row's heaviest loses bits, and below 2^-36
+ * counts as 0.
+ * dt          type of q and out: the cache's, or APC_F16 / APC_BF16 where the
+ *             cache is APC_E4M3.
+ * t           rows of q and out; t <= APC_MAX_TOKENS, t * q_heads <= APC_MAX_PROMPT_ROWS.
+ * q, out      row i's head a at i * row + a * head elements (strides q_row,
+ *             q_head, out_row, out_head >= 0; d contiguous).
+ * starts      b + 1 int32 (device), not falling, from 0 to t (cut to these;
+ *             a sequence whose end is not above its start has no row).  Rows of
+ *             out and lse outside all sequences stay as they were.
+ * q_heads     a multiple of the cache's heads; b * q_heads <= APC_MAX_ATTEND_ROWS.
+ * pages       b x max_pages int32 page numbers at row stride ld_pages;
+ *             max_pages * page <= APC_MAX_TOKENS.
+ * lengths     b int32.
+ * prefix      b int32, or NULL: no prefix.
+ * slopes      q_heads float32, or NULL: no bias.
+ * window      >= 0 (0: none).   cap: finite, >= 0 (0: none).   scale: finite.
+ * lse         t x q_heads float32, or NULL.
+ * ws          workspace of at least apc_attend_prompt_workspace() bytes (16-byte
+ *             aligned); nothing in it needs to start at zero.
+ * b = 0 and t = 0 are no-ops.  Errors: APC_E_ARG, APC_E_DTYPE, APC_E_WORKSPACE.
+ * Asynchronous on stream.
+ */
+apc_status apc_attend_prompt(const apc_kv* c /* host */, apc_dtype dt, int64_t t, const void* q, int64_t q_row,
+                             int64_t q_head, int32_t b, const int32_t* starts, int32_t q_heads, const int32_t* pages,
+                             int32_t max_pages, int64_t ld_pages, const int32_t* lengths, const int32_t* prefix,
+                             const float* slopes, int32_t window, float cap, float scale, void* out, int64_t out_row,
+                             int64_t out_head, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Measurement hook (for benchmarks and profilers, not for the method):

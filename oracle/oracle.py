@@ -631,3 +631,82 @@ def attend(dtype: str, q, k: np.ndarray, v: np.ndarray, k_scale, v_scale, pages,
                 spread[i, a] = w @ np.abs(vv) / w.sum()
                 top[i, a] = abs(scale) * (np.abs(kk) @ np.abs(q[i, a])).max()
     return out, lse, spread, top
+
+
+def rotary_freqs(rot: int, base: float, factor: float, original: float, low: float, high: float) -> np.ndarray:
+    """Angle of one position for each of rot / 2 pairs, in a context `factor` times the `original` one."""
+    f = np.float64(base) ** (-2.0 * np.arange(rot // 2) / rot)
+    turns = original * f / (2.0 * np.pi)
+    g = np.clip((turns - low) / (high - low), 0.0, 1.0) if original > 0 else np.zeros_like(f)
+    return g * f + (1.0 - g) * f / factor
+
+
+def rotate(x, positions, freq, interleaved: bool, mag: float = 1.0):
+    """t x heads x d rows, their first 2 len(freq) elements turned pair by pair; rows of negative positions as they are."""
+    y = np.array(x, dtype=np.float64)
+    n = len(freq)
+    a, b = (np.arange(n) * 2, np.arange(n) * 2 + 1) if interleaved else (np.arange(n), np.arange(n) + n)
+    for i, p in enumerate(np.asarray(positions, dtype=np.int64)):
+        if p < 0:
+            continue
+        w = np.float64(p) * np.asarray(freq, dtype=np.float64)
+        u, v = y[i][:, a].copy(), y[i][:, b].copy()
+        y[i][:, a] = mag * (u * np.cos(w) - v * np.sin(w))
+        y[i][:, b] = mag * (v * np.cos(w) + u * np.sin(w))
+    return y
+
+
+def attend_prompt(dtype: str, q, starts, k: np.ndarray, v: np.ndarray, k_scale, v_scale, pages, lengths, scale: float,
+                  window: int = 0, cap: float = 0.0, slopes=None, prefix=None):
+    """(out, lse, spread, top, heavy, away) in float64.  q: t x q_heads x d values, sequence i's rows from starts[i] to
+    starts[i + 1].  spread and top as of attend(); heavy = the largest |v_j| / sum_j exp(s_j - max s) per output element
+    (what a lost weight costs), away = the largest |p - j| of a row.  Rows of no sequence: NaN."""
+    n_pages, heads, page, d = k.shape
+    q = np.asarray(q, dtype=np.float64)
+    t, hq, _ = q.shape
+    group = hq // heads
+    out, spread, heavy = (np.full((t, hq, d), np.nan) for _ in range(3))
+    lse, top, away = (np.full((t, hq), np.nan) for _ in range(3))
+    for i in range(len(lengths)):
+        r0, r1 = (min(max(int(starts[i + e]), 0), t) for e in (0, 1))
+        if r1 <= r0:
+            continue
+        n = min(max(int(lengths[i]), 0), pages.shape[1] * page)
+        at = n - (r1 - r0) + np.arange(r1 - r0)
+        j = np.arange(n)
+        p = pages[i][j // page].astype(np.int64) if n else np.zeros(0, np.int64)
+        j, p = j[(p >= 0) & (p < n_pages)], p[(p >= 0) & (p < n_pages)]
+        dist = np.abs(at[:, None] - j)
+        seen = j <= at[:, None]
+        if prefix is not None:
+            seen |= j < int(prefix[i])
+        if window:
+            seen &= dist < window
+        out[r0:r1], spread[r0:r1], heavy[r0:r1], lse[r0:r1], top[r0:r1], away[r0:r1] = 0, 0, 0, -np.inf, 0, 0
+        if j.size == 0:
+            continue
+        away[r0:r1] = np.where(seen, dist, 0).max(axis=1)[:, None]
+        for h in range(heads):
+            kk, vv = kv_values(dtype, k[p, h, j % page]), kv_values(dtype, v[p, h, j % page])
+            if k_scale is not None:
+                kk = kk * k_scale[p, h, j % page].astype(np.float64)[:, None]
+                vv = vv * v_scale[p, h, j % page].astype(np.float64)[:, None]
+            for a in range(h * group, (h + 1) * group):
+                s = scale * (q[r0:r1, a] @ kk.T)
+                if cap > 0:
+                    s = cap * np.tanh(s / cap)
+                if slopes is not None:
+                    s = s - float(slopes[a]) * dist
+                s = np.where(seen, s, -np.inf)
+                m = s.max(axis=1, keepdims=True)
+                some = np.isfinite(m[:, 0])
+                w = np.exp(s - np.where(np.isfinite(m), m, 0.0))
+                total = np.where(some, w.sum(axis=1), 1.0)[:, None]
+                with np.errstate(divide="ignore"):
+                    lse[r0:r1, a] = np.where(some, m[:, 0] + np.log(w.sum(axis=1)), -np.inf)
+                out[r0:r1, a] = w @ vv / total
+                spread[r0:r1, a] = w @ np.abs(vv) / total
+                heavy[r0:r1, a] = np.abs(vv).max(axis=0) / total * some[:, None]
+                big = abs(scale) * (np.abs(q[r0:r1, a]) @ np.abs(kk).T)
+                top[r0:r1, a] = np.where(seen, big, 0).max(axis=1)
+    return out, lse, spread, top, heavy, away

@@ -40,6 +40,12 @@ class _KvStruct(ctypes.Structure):
                 ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
+class _RotaryStruct(ctypes.Structure):
+    """apc_rotary of include/apc.h."""
+    _fields_ = [("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("mag", ctypes.c_float),
+                ("freq", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -108,6 +114,16 @@ def load() -> ctypes.CDLL:
     L.apc_attend.argtypes = [kv, ctypes.c_int, vp, i64, i64, i32, i32, vp, i32, i64, vp, i32, f32, vp, i64, i64, vp, vp,
                              sz, vp]
     L.apc_attend.restype = st
+    f64 = ctypes.c_double
+    L.apc_rotary_freqs.argtypes = [i32, f64, f64, f64, f64, f64, vp]
+    L.apc_rotary_freqs.restype = st
+    L.apc_rotate.argtypes = [ctypes.POINTER(_RotaryStruct), ctypes.c_int, i64, i32, i32, vp, i64, i64, vp, vp, i64, i64, vp]
+    L.apc_rotate.restype = st
+    L.apc_attend_prompt_workspace.argtypes = [kv, i64, i32, i32, i32, ctypes.POINTER(sz)]
+    L.apc_attend_prompt_workspace.restype = st
+    L.apc_attend_prompt.argtypes = [kv, ctypes.c_int, i64, vp, i64, i64, i32, vp, i32, vp, i32, i64, vp, vp, vp, i32, f32,
+                                    f32, vp, i64, i64, vp, vp, sz, vp]
+    L.apc_attend_prompt.restype = st
     L.apc_set_kernel_events.argtypes = [vp, vp]
     L.apc_set_kernel_events.restype = st
     L.apc_status_str.argtypes = [ctypes.c_int]
@@ -509,5 +525,99 @@ def apc_attend(c: KvCache, q: torch.Tensor, pages: torch.Tensor, lengths: torch.
     rc = load().apc_attend(c.ref, _dtype(q, "q"), qp, qs[0], qs[1], b, q_heads, pp, max_pages,
                            ps[0] if b > 1 else max_pages, lp, window, scale, op, os_[0], os_[1], ep, _ptr(ws),
                            ws.numel() * ws.element_size(), _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def _on_device(*tensors: Optional[torch.Tensor]):
+    """The kernels run on the current device: all of the call's tensors have to be there."""
+    here = torch.cuda.current_device() if _device is None else _device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"expected tensors on the current device (cuda:{here}), got one on {t.device}")
+
+
+class Rotary:
+    """Rotary positions: freq the angle of one position for each pair (device float64, as apc_rotary_freqs gives them),
+    interleaved whether pairs are neighbours or halves, mag a factor of what is turned.  Keeps the tensor alive."""
+
+    def __init__(self, freq: torch.Tensor, interleaved: bool = False, mag: float = 1.0):
+        if freq.dim() != 1 or freq.dtype != torch.float64 or not freq.is_contiguous():
+            raise ValueError("freq must be a contiguous 1-D float64 tensor")
+        self.freq, self.rot = freq, 2 * freq.shape[0]
+        self.struct = _RotaryStruct(self.rot, int(interleaved), mag, _ptr(freq))
+        self.ref = ctypes.byref(self.struct)
+
+
+def apc_rotary_freqs(rot: int, base: float = 10000.0, factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                     high: float = 4.0) -> np.ndarray:
+    """Frequencies (float64, rot / 2) of rotary positions, for a context `factor` times the `original` one."""
+    freq = np.zeros(max(rot, 0) // 2, dtype=np.float64)
+    _check(load().apc_rotary_freqs(rot, base, factor, original, low, high, freq.ctypes.data))
+    return freq
+
+
+def apc_rotate(r: Rotary, x: torch.Tensor, positions: torch.Tensor, out: torch.Tensor, stream=None):
+    """Rows of heads (x and out t x heads x d, tokens and heads strided as they come; out may be x) turned by their
+    tokens' positions (t int32; negative: left out)."""
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 3:
+        raise ValueError("x must be a t x heads x d tensor")
+    t, heads, d = shape
+    xp, xs = _view(x, "x", shape, dtype)
+    op, os_ = _view(out, "out", shape, dtype)
+    pp, _ = _view(positions, "positions", (t,), torch.int32)
+    _on_device(x, out, positions, r.freq)
+    # of one token or head, torch's stride may be anything
+    rc = load().apc_rotate(r.ref, _dtype(x, "x"), t, heads, d, xp, xs[0], xs[1], pp, op, os_[0] if t > 1 else heads * d,
+                           os_[1] if heads > 1 else d, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def apc_attend_prompt_workspace(c: KvCache, t: int, b: int, q_heads: int, max_pages: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load().apc_attend_prompt_workspace(c.ref, t, b, q_heads, max_pages, ctypes.byref(n)))
+    return n.value
+
+
+def attend_prompt_workspace_tensor(c: KvCache, t: int, b: int, q_heads: int, max_pages: int, device=None) -> torch.Tensor:
+    """Device buffer of apc_attend_prompt_workspace() bytes (torch allocations are 256-byte aligned)."""
+    return torch.empty(max(apc_attend_prompt_workspace(c, t, b, q_heads, max_pages), 256), dtype=torch.uint8,
+                       device=device or "cuda")
+
+
+def apc_attend_prompt(c: KvCache, q: torch.Tensor, starts: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor,
+                      scale: float, out: torch.Tensor, ws: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                      window: int = 0, cap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                      prefix: Optional[torch.Tensor] = None, stream=None):
+    """Attention of several new tokens per sequence: q and out t x q_heads x d, sequence i's rows from starts[i] to
+    starts[i + 1] (b + 1 int32), pages b x max_pages int32 (rows may be strided), lengths b int32 (all tokens, the new
+    ones among them), prefix b int32 or None, slopes q_heads float32 or None, lse t x q_heads float32 or None."""
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 3 or pages.dim() != 2:
+        raise ValueError("q must be a t x q_heads x d tensor and pages a b x max_pages int32 tensor")
+    t, q_heads, d = shape
+    b, max_pages = pages.shape
+    if d != c.d:
+        raise ValueError(f"q has {d} elements a head and the cache {c.d}")
+    qp, qs = _view(q, "q", shape, dtype)
+    op, os_ = _view(out, "out", shape, dtype)
+    sp, _ = _view(starts, "starts", (b + 1,), torch.int32)
+    pp, ps = _view(pages, "pages", (b, max_pages), torch.int32)
+    lp, _ = _view(lengths, "lengths", (b,), torch.int32)
+    ep = fp = bp = None
+    if lse is not None:
+        if not lse.is_contiguous():
+            raise ValueError("lse: expected a contiguous tensor")
+        ep, _ = _view(lse, "lse", (t, q_heads), torch.float32)
+    if prefix is not None:
+        fp, _ = _view(prefix, "prefix", (b,), torch.int32)
+    if slopes is not None:
+        bp, _ = _view(slopes, "slopes", (q_heads,), torch.float32)
+    _on_device(q, out, starts, pages, lengths, lse, prefix, slopes, ws, c.k)
+    rc = load().apc_attend_prompt(c.ref, _dtype(q, "q"), t, qp, qs[0], qs[1], b, sp, q_heads, pp, max_pages,
+                                  ps[0] if b > 1 else max_pages, lp, fp, bp, window, cap, scale, op, os_[0], os_[1], ep,
+                                  _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
     if rc:
         _check(rc)

@@ -775,4 +775,116 @@ apc_status apc_attend(const apc_kv* c, apc_dtype dt, const void* q, int64_t q_ro
     return ok();
 }
 
+apc_status apc_rotary_freqs(int32_t rot, double base, double factor, double original, double low, double high,
+                            double* freq)
+{
+    if (rot < 2 || rot > APC_MAX_HEAD_DIM || rot % 2 != 0)
+        return fail(APC_E_ARG, "apc_rotary_freqs: rot must be even, from 2 to %d (rot=%d)", APC_MAX_HEAD_DIM, rot);
+    auto good = [](double x) { return std::isfinite(x) && x > 0.0; };
+    if (!good(base) || !good(factor) || !std::isfinite(original) || original < 0.0)
+        return fail(APC_E_ARG, "apc_rotary_freqs: base and factor must be finite and > 0, original finite and >= 0");
+    if (original > 0.0 && (!std::isfinite(low) || !std::isfinite(high) || !(high > low)))
+        return fail(APC_E_ARG, "apc_rotary_freqs: low and high must be finite and high > low");
+    if (!freq) return fail(APC_E_ARG, "apc_rotary_freqs: freq is NULL");
+    const double two_pi = 6.283185307179586476925;
+    for (int i = 0; i < rot / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot);
+        double g = 0.0;
+        if (original > 0.0) {
+            g = (original * f / two_pi - low) / (high - low);
+            g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
+        }
+        freq[i] = g * f + (1.0 - g) * f / factor;
+    }
+    return ok();
+}
+
+apc_status apc_rotate(const apc_rotary* r, apc_dtype dt, int64_t t, int32_t heads, int32_t d, const void* x, int64_t x_tok,
+                      int64_t x_head, const int32_t* positions, void* out, int64_t out_tok, int64_t out_head, void* stream)
+{
+    if (!r) return fail(APC_E_ARG, "apc_rotate: NULL description");
+    if (!float_dtype(dt)) return fail(APC_E_DTYPE, "apc_rotate: rows are f32, f16 or bf16 (got %d)", (int)dt);
+    if (d < 1 || d > APC_MAX_HEAD_DIM || r->rot < 2 || r->rot > d || r->rot % 2 != 0)
+        return fail(APC_E_ARG, "apc_rotate: need d <= %d and an even rot from 2 to d (d=%d rot=%d)", APC_MAX_HEAD_DIM, d,
+                    r->rot);
+    if (r->interleaved != 0 && r->interleaved != 1) return fail(APC_E_ARG, "apc_rotate: interleaved must be 0 or 1");
+    if (!std::isfinite(r->mag)) return fail(APC_E_ARG, "apc_rotate: mag is not finite");
+    if (heads < 1 || t < 0 || t > (int64_t)INT32_MAX / heads)
+        return fail(APC_E_ARG, "apc_rotate: need heads >= 1 and 0 <= t * heads < 2^31 (t=%lld heads=%d)", (long long)t, heads);
+    if (x_tok < 0 || x_head < 0 || out_tok < 0 || out_head < 0) return fail(APC_E_ARG, "apc_rotate: negative stride");
+    if (t == 0) return ok();
+    const int e = apc::elem_bytes(dt);
+    if (!x || !out || !positions || !r->freq || !aligned_to(x, e) || !aligned_to(out, e) || !aligned_to(positions, 4) ||
+        !aligned_to(r->freq, 8))
+        return fail(APC_E_ARG, "apc_rotate: x, out, positions and freq must be device pointers aligned to their elements");
+    // rows of out that share elements would be written by several threads
+    if ((heads > 1 && out_head < d) || (t > 1 && out_tok < d) || (heads > 1 && t > 1 && out_head == out_tok))
+        return fail(APC_E_ARG, "apc_rotate: rows of out overlap");
+    const apc::RotateArgs a{x, out, positions, r->freq, t, x_tok, x_head, out_tok, out_head, heads, d, r->rot, r->mag,
+                            r->interleaved != 0, false};
+    hipError_t err = apc::launch_rotate(dt, a, static_cast<hipStream_t>(stream));
+    if (err != hipSuccess) return hip_fail(err, "apc_rotate launch");
+    return ok();
+}
+
+static apc_status check_attend_prompt(const char* who, const apc_kv* c, int64_t t, int32_t b, int32_t q_heads,
+                                      int32_t max_pages)
+{
+    if (apc_status st = check_kv(who, c)) return st;
+    // (the kernel counts a sequence's rows in 32 bits, and a launch has fewer than 2^32 threads)
+    if (b < 0 || q_heads < 1 || q_heads % c->heads != 0 || (int64_t)b * q_heads > APC_MAX_ATTEND_ROWS)
+        return fail(APC_E_ARG, "%s: need b >= 0, q_heads a multiple of the cache's %d heads and b * q_heads <= %d "
+                    "(b=%d q_heads=%d)", who, c->heads, APC_MAX_ATTEND_ROWS, b, q_heads);
+    if (t < 0 || t > APC_MAX_TOKENS || t * q_heads > APC_MAX_PROMPT_ROWS)
+        return fail(APC_E_ARG, "%s: need 0 <= t <= %d and t * q_heads <= %d (t=%lld q_heads=%d)", who, APC_MAX_TOKENS,
+                    APC_MAX_PROMPT_ROWS, (long long)t, q_heads);
+    if (max_pages < 0 || max_pages > APC_MAX_TOKENS / c->page)
+        return fail(APC_E_ARG, "%s: need 0 <= max_pages * page <= %d (max_pages=%d)", who, APC_MAX_TOKENS, max_pages);
+    return APC_OK;
+}
+
+apc_status apc_attend_prompt_workspace(const apc_kv* c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages,
+                                       size_t* bytes)
+{
+    if (!bytes) return fail(APC_E_ARG, "apc_attend_prompt_workspace: bytes is NULL");
+    if (apc_status st = check_attend_prompt("apc_attend_prompt_workspace", c, t, b, q_heads, max_pages)) return st;
+    *bytes = apc::prompt_workspace(*c, t, b, q_heads, max_pages);
+    return ok();
+}
+
+apc_status apc_attend_prompt(const apc_kv* c, apc_dtype dt, int64_t t, const void* q, int64_t q_row, int64_t q_head,
+                             int32_t b, const int32_t* starts, int32_t q_heads, const int32_t* pages, int32_t max_pages,
+                             int64_t ld_pages, const int32_t* lengths, const int32_t* prefix, const float* slopes,
+                             int32_t window, float cap, float scale, void* out, int64_t out_row, int64_t out_head,
+                             float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    if (apc_status st = check_attend_prompt("apc_attend_prompt", c, t, b, q_heads, max_pages)) return st;
+    if ((dt != APC_F16 && dt != APC_BF16) || (c->dt != APC_E4M3 && dt != c->dt))
+        return fail(APC_E_DTYPE, "apc_attend_prompt: queries are of the cache's type, or f16 or bf16 over e4m3 (got %d)",
+                    (int)dt);
+    if (window < 0) return fail(APC_E_ARG, "apc_attend_prompt: window < 0");
+    if (!std::isfinite(scale)) return fail(APC_E_ARG, "apc_attend_prompt: scale is not finite");
+    if (!(cap >= 0.f) || !std::isfinite(cap)) return fail(APC_E_ARG, "apc_attend_prompt: cap must be finite and >= 0");
+    if (q_row < 0 || q_head < 0 || out_row < 0 || out_head < 0 || ld_pages < max_pages)
+        return fail(APC_E_ARG, "apc_attend_prompt: negative stride, or ld_pages < max_pages");
+    if (b == 0 || t == 0) return ok();
+    if (!q || !out || !starts || !lengths || (max_pages > 0 && !pages) || !aligned_to(q, 2) || !aligned_to(out, 2) ||
+        !aligned_to(starts, 4) || !aligned_to(pages, 4) || !aligned_to(lengths, 4) || !aligned_to(prefix, 4) ||
+        !aligned_to(slopes, 4) || !aligned_to(lse, 4))
+        return fail(APC_E_ARG, "apc_attend_prompt: q, out, starts, lengths and pages must be device pointers, all aligned to "
+                    "their elements");
+    const size_t need = apc::prompt_workspace(*c, t, b, q_heads, max_pages);
+    if (need > 0 && (!ws || !aligned16(ws)))
+        return fail(APC_E_ARG, "apc_attend_prompt: workspace must be a non-NULL 16-byte aligned device pointer");
+    if (ws_bytes < need)
+        return fail(APC_E_WORKSPACE, "apc_attend_prompt: workspace of %zu bytes, %zu needed", ws_bytes, need);
+    // (positions are below 2^30, and no window beyond all of them differs from none)
+    const int32_t within = window < APC_MAX_TOKENS ? window : 0;
+    const apc::PromptArgs a{q, out, starts, pages, lengths, prefix, slopes, lse, ws, t, q_row, q_head, out_row, out_head,
+                            ld_pages, b, q_heads, max_pages, within, scale, cap};
+    hipError_t err = apc::launch_attend_prompt(dt, *c, a, static_cast<hipStream_t>(stream));
+    if (err != hipSuccess) return hip_fail(err, "apc_attend_prompt launch");
+    return ok();
+}
+
 }  // extern "C"

@@ -84,6 +84,45 @@ struct AttendPlan {
 size_t attend_workspace(const apc_kv& c, int32_t b, int32_t q_heads, int32_t max_pages);
 hipError_t launch_attend(int dt, const apc_kv& c, const AttendArgs& a, hipStream_t s);
 
+// positions of rows of heads (rotate.hip)
+struct RotateArgs {
+    const void* x;
+    void* out;
+    const int32_t* positions;
+    const double* freq;
+    int64_t t, x_tok, x_head, out_tok, out_head;    // strides in elements
+    int32_t heads, d, rot;
+    float mag;
+    bool interleaved, past;                         // past: outputs go past the caches
+};
+hipError_t launch_rotate(int dt, const RotateArgs& a, hipStream_t s);
+
+struct PromptArgs {
+    const void* q;
+    void* out;
+    const int32_t *starts, *pages, *lengths, *prefix;
+    const float* slopes;
+    float* lse;
+    void* ws;
+    int64_t t, q_row, q_head, out_row, out_head, ld_pages;
+    int32_t b, q_heads, max_pages, window;
+    float scale, cap;
+};
+struct PromptPlan {
+    int32_t shift;       // log2 of the page
+    int32_t dp;          // elements of a head that the kernel computes with
+    int32_t rows;        // of a row tile: 32 or 128
+    int32_t tiles;       // row tiles of a key-value head, at most
+    int32_t splits;      // parts of a unit's keys, at most
+    int32_t min_tiles;   // tiles of keys of a part, at least
+    float to_cap;        // from scores in units of log2 to the tanh's argument
+};
+size_t prompt_workspace(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages);
+hipError_t launch_attend_prompt(int dt, const apc_kv& c, const PromptArgs& a, hipStream_t s);
+hipError_t launch_prompt_f16(const apc_kv& c, const PromptArgs& a, const PromptPlan& p, hipStream_t s);
+hipError_t launch_prompt_bf16(const apc_kv& c, const PromptArgs& a, const PromptPlan& p, hipStream_t s);
+hipError_t launch_prompt_e4m3(int dt, const apc_kv& c, const PromptArgs& a, const PromptPlan& p, hipStream_t s);
+
 // factor layout of a cache: n rounded up to a multiple of 256 factors, zeros past n
 __host__ __device__ inline int64_t factor_pad(int64_t n) { return (n + 255) / 256 * 256; }
 

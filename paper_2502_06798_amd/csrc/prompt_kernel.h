@@ -1,0 +1,660 @@
+// Attention of several new tokens of each sequence over a paged key-value
+// cache: the kernel, built for one cache type by each of prompt_*.hip.
+//
+// The new tokens of a sequence and the query heads that share a key-value head
+// make rows (token by token), cut into tiles of M rows; a row tile of a
+// key-value head is a unit, a workgroup's work.  Long units that are few are cut
+// along the keys as well, and k_prompt_join (prompt.hip) joins the parts.
+//
+// Keys and values go through LDS, 16 bits each: from e4m3 exactly, the scales
+// beside them.  Per wave of 32 rows and tile of KT keys, in matrix instructions of
+// 32 x 32 x 16:
+//   S^T = K Q^T    keys are the rows, query rows the columns: a lane holds half
+//                  of one query row's scores, the other lane half the rest.
+//   P   = exp2(S - m), float32; m is the row's running maximum, raised (and the
+//                  sums scaled) only where a score passes it by SLACK, so that a
+//                  tile needs no exchange between lanes as a rule.
+//   O^T += V^T P^T the lane's weights are the second operand as they stand, given
+//                  that the first operand's lanes hold the values of the same
+//                  keys, which LDS reads that transpose 4 x 16 elements give.
+// Two shapes: SHARED, where R waves have 32 rows each and the same keys (tiles in
+// two LDS buffers, the next on its way in registers); else KW waves have the same
+// 32 rows and every KW-th tile each, in an LDS buffer of their own.
+#pragma once
+
+#include "attend_common.h"
+
+#include <cmath>
+#include <type_traits>
+
+namespace apc {
+
+using f32x16 = float __attribute__((ext_vector_type(16)));
+using s16x4 = short __attribute__((ext_vector_type(4)));
+
+// 32 x 32 x 16: D = A B + C; a lane's 8 values of A are row lane % 32, of B
+// column lane % 32, both at k = 8 (lane / 32); of D column lane % 32, row
+// 8 (r / 4) + 4 (lane / 32) + r % 4
+template <bool BF> __device__ inline f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c)
+{
+    if constexpr (BF)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// 16 lanes read 4 rows of 16 elements, lane i the elements 4 (i % 4) on of row
+// i / 4, and get columns: lane i element i of the four rows
+__device__ inline uint2 read_columns(const uint16_t* lds)
+{
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4*)(const_cast<uint16_t*>(lds))));
+}
+
+// over the two lanes that have a query row
+__device__ inline float both_halves_max(float x)
+{
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __builtin_fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ inline float both_halves_sum(float x)
+{
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
+
+// the halves of w that hold +inf (kind 0), -inf (1) or NaN (2), each as 1
+template <bool BF> __device__ inline uint32_t is_kind(uint32_t w, int kind)
+{
+    constexpr uint32_t INF = BF ? 0x7f80u : 0x7c00u, ONE = BF ? 0x3f80u : 0x3c00u;
+    const uint32_t lo = w & 0xffffu, hi = w >> 16;
+    auto is = [&](uint32_t x) { return kind == 0 ? x == INF : kind == 1 ? x == (INF | 0x8000u) : (x & 0x7fffu) > INF; };
+    return (is(lo) ? ONE : 0u) | (is(hi) ? ONE << 16 : 0u);
+}
+
+// tanh(x) / x for |x| <= NEAR from x^2, within 2^-23 (a polynomial fitted to the
+// smallest largest relative error)
+constexpr float NEAR = 0.625f;
+__device__ inline float tanh_over_x(float z)
+{
+    float r = __builtin_fmaf(z, -0.0056599868f, 0.020590985f);
+    r = __builtin_fmaf(z, r, -0.053721067f);
+    r = __builtin_fmaf(z, r, 0.13331127f);
+    r = __builtin_fmaf(z, r, -0.3333326f);
+    return __builtin_fmaf(z, r, 1.0f);
+}
+
+// a row tile of a sequence: the sequence's first row among the new tokens', their number, the tile
+struct PromptUnit { int seq, first, n, tile; };
+
+// The k-th of all sequences' row tiles of `rows` rows, found by every wave for
+// itself, 256 sequences a step.  The last tiles of a sequence come first: where
+// tokens see what stands before them, they have most to do.
+__device__ INLINE inline PromptUnit prompt_unit(const PromptArgs& a, int group, int rows, int k)
+{
+    const int lane = threadIdx.x & 63, t = (int)a.t;
+    for (int seq0 = 0; seq0 < a.b; seq0 += 256) {
+        int first[4], n[4], tiles[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = seq0 + 64 * u + lane;
+            int from = 0, to = 0;
+            if (i < a.b) from = a.starts[i], to = a.starts[i + 1];
+            from = from < 0 ? 0 : from < t ? from : t;
+            to = to < 0 ? 0 : to < t ? to : t;
+            first[u] = from;
+            n[u] = to > from ? to - from : 0;
+            tiles[u] = (int)(((int64_t)n[u] * group + rows - 1) / rows);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (seq0 + 64 * u >= a.b) break;
+            int upto = tiles[u];
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int o = __shfl_up(upto, d, 64);
+                if (lane >= d) upto += o;
+            }
+            const int total = __builtin_amdgcn_readlane(upto, 63);
+            if (k < total) {
+                const int l = __builtin_ctzll(__ballot(upto > k));
+                return PromptUnit{seq0 + 64 * u + l, __builtin_amdgcn_readlane(first[u], l), __builtin_amdgcn_readlane(n[u], l),
+                                  __builtin_amdgcn_readlane(upto, l) - 1 - k};
+            }
+            k -= total;
+        }
+    }
+    return PromptUnit{-1, 0, 0, 0};
+}
+
+// What the rows of a sequence see: the tokens [first(p), end(p)) of the one at position p.  Both never fall as p rises.
+struct PromptSight {
+    int len, past, prefix, window, group;
+    __device__ INLINE PromptSight(const PromptArgs& a, int shift, int group, const PromptUnit& u) : window(a.window), group(group)
+    {
+        const int32_t held = table_entry(a.lengths, u.seq), cap = a.max_pages << shift;
+        len = held < 0 ? 0 : held < cap ? held : cap;
+        past = len - u.n;                                       // position of the first new token
+        prefix = a.prefix ? table_entry(a.prefix, u.seq) : 0;
+    }
+    __device__ INLINE int position(int row) const { return past + row / group; }
+    __device__ INLINE int first(int p) const { return window > 0 && p >= window ? p + 1 - window : 0; }
+    __device__ INLINE int end(int p) const
+    {
+        int e = p + 1 > prefix ? p + 1 : prefix;
+        if (window > 0 && e > p + window) e = p + window;
+        return e < len ? e : len;
+    }
+};
+
+// A unit's tiles of kt keys, and into how many parts they are cut
+struct PromptKeys {
+    int tile0, tiles, parts;
+    __device__ INLINE PromptKeys(const PromptPlan& p, const PromptSight& s, const PromptUnit& u, int rows, int kt)
+    {
+        const int r0 = u.tile * rows, all = u.n * s.group, r1 = r0 + rows < all ? r0 + rows : all;
+        const int lo = s.first(s.position(r0)), hi = s.end(s.position(r1 - 1));
+        tile0 = lo / kt;
+        tiles = hi > lo ? (hi + kt - 1) / kt - tile0 : 0;
+        const int most = tiles / p.min_tiles;
+        parts = most < 1 ? 1 : most < p.splits ? most : p.splits;
+    }
+};
+
+// partial results in the workspace: sums (float32, padded d a row), then each row's maximum and sum of weights
+__host__ __device__ inline int64_t prompt_slots(const PromptPlan& p, int heads) { return (int64_t)p.tiles * heads * p.splits * p.rows; }
+__device__ inline int64_t prompt_slot(const PromptPlan& p, int heads, int k, int head, int part)
+{
+    return (((int64_t)k * heads + head) * p.splits + part) * p.rows;
+}
+
+template <int DT, int CDT, int DP, int R, int KW>
+__global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt(apc_kv c, PromptArgs a, PromptPlan p)
+{
+    static_assert(R == 1 || KW == 1);
+    using T = typename Elem<DT>::T;
+    constexpr bool E8 = CDT == APC_E4M3, QBF = DT == APC_BF16, SHARED = R > 1;
+    // The weights' type is the values': f16 over f16, else bf16 (e4m3 weights have the
+    // value's scale in them, which can leave f16's range).  One part of a weight
+    // loses up to half a step of it, 2^-11 or 2^-8, as much as the output's rounding
+    // to the same type, and in sums over many values no more.  A second part, the
+    // rounded rest, is taken where the waves share the keys out, whose time is the
+    // keys' and values' loads, and by f16 queries over e4m3, whose outputs are f16.
+    constexpr bool PBF = QBF || E8, TWO = !SHARED || PBF != QBF;
+    // f16 weights end at 2^-24 and are whole from 2^-14 on: the row's heaviest stands at
+    // 2^OFF to 2^15, so weights from 2^-26 of it are whole and those below 2^-36 are left out.
+    constexpr float SLACK = PBF ? 8.f : 3.f, OFF = PBF ? 0.f : 12.f;
+    constexpr int M = 32 * R, ES = E8 ? 1 : 2;
+    constexpr int KT = SHARED && DP <= 128 ? 64 : 32, G = KT / 16;  // keys of a tile, sixteens of them (no page is smaller)
+    constexpr int NT = SHARED ? 64 * R : 64;                    // threads that load a tile
+    constexpr int CH = DP * ES / 16, RW = 64 / CH;              // 16-byte pieces of a row, rows of a wave's load
+    constexpr int ITS = KT * CH / NT, STEP = NT / CH;           // loads of a thread, rows between them
+    constexpr int KS = DP + 8, VS = DP + 16;                    // elements between rows in LDS
+    constexpr int BUF = KT * (KS + VS) + (E8 ? 4 * KT : 0);     // of a buffer (16 bits each)
+    constexpr int BUFS = SHARED ? 2 : KW;
+    constexpr int JOIN = SHARED ? 0 : KW * (32 * (DP + 4) + 64) * 2;
+    static_assert(RW <= 16 && KT * CH % NT == 0);
+    __shared__ __attribute__((aligned(16))) uint16_t lds[BUFS * BUF > JOIN ? BUFS * BUF : JOIN];
+
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = a.q_heads / c.heads;
+    // a key-value head's units on one XCD, where the heads are a multiple of 8 (workgroups go round over the XCDs)
+    const int head = blockIdx.x % c.heads, k = blockIdx.x / c.heads / p.splits, part = blockIdx.x / c.heads % p.splits;
+    const PromptUnit u = prompt_unit(a, group, M, k);
+    if (u.seq < 0) return;
+    const PromptSight sight(a, p.shift, group, u);
+    const PromptKeys keys(p, sight, u, M, KT);
+    if (part >= keys.parts) return;
+    const int all = u.n * group, len = sight.len;
+
+    // this wave's rows, and this lane's
+    const int row0 = u.tile * M + (SHARED ? wave * 32 : 0);
+    const bool busy = row0 < all;
+    const int rowz = row0 + 31 < all ? row0 + 31 : all - 1;
+    const int pa = sight.position(busy ? row0 : rowz), pz = sight.position(rowz);
+    const int lo_a = sight.first(pa), lo_z = sight.first(pz), hi_a = sight.end(pa), hi_z = sight.end(pz);
+    const int row = row0 + col < all ? row0 + col : all - 1;
+    const int token = row / group, qh = head * group + row % group;
+    const int at = sight.past + token, lo = sight.first(at), hi = sight.end(at);
+
+    const int row_bytes = c.d * ES, in_page = c.page - 1;
+    u32x4 q[DP / 16];
+    {
+        const T* from = static_cast<const T*>(a.q) + (u.first + token) * a.q_row + qh * a.q_head + 8 * half;
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u; // scores are multiplied by |scale|
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            q[s] = u32x4{0, 0, 0, 0};
+            if (s * 16 < c.d) __builtin_memcpy(&q[s], from + s * 16, 16);
+            q[s] ^= flip;
+        }
+    }
+    const float sc = __builtin_fabsf(a.scale) * LOG2E;
+    const float slope = a.slopes ? a.slopes[qh] * LOG2E : 0.f;
+
+    // keys and values on their way: 16-byte pieces of rows, zeros where there is no row
+    const int32_t* table = a.pages + u.seq * a.ld_pages;
+    const int last_page = (len - 1) >> p.shift;
+    const int r_lane = lane / CH, ch = lane % CH;
+    const int s_key = SHARED ? lane % KT : lane & 31;           // whose scale the lane loads
+    auto row_of = [&](int it) INLINE { return it * STEP + (SHARED ? wave * RW : 0); };
+    struct Pages { int32_t id[G], own[ITS], scale; };           // of the sixteens, of the thread's rows, of its scale
+    auto find = [&](int j0) INLINE {
+        Pages pg;
+        auto index = [&](int j) INLINE { return j >> p.shift < last_page ? j >> p.shift : last_page; };
+#pragma unroll
+        for (int g = 0; g < G; ++g) pg.id[g] = table_entry(table, index(j0 + 16 * g));
+#pragma unroll
+        for (int it = 0; it < ITS; ++it) pg.own[it] = SHARED ? table_entry(table, index(j0 + row_of(it))) : pg.id[it * STEP / 16];
+        pg.scale = E8 ? table[index(j0 + s_key)] : 0;
+        return pg;
+    };
+    auto there = [&](int32_t id, int j) INLINE { return (uint32_t)id < (uint64_t)c.n_pages && j < len; };
+    auto first_row = [&](int32_t id, int j) INLINE { return (((int64_t)id * c.heads + head) << p.shift) + (j & in_page); };
+    const bool in_row = ch * 16 < row_bytes;
+    struct Tile { u32x4 k[ITS], v[ITS]; float scale; };
+    auto load = [&](Tile& to, int j0, const Pages& pg) INLINE {
+#pragma unroll
+        for (int it = 0; it < ITS; ++it) {
+            const int r0 = row_of(it), j = j0 + r0 / 16 * 16;
+            const int32_t id = pg.own[it];
+            to.k[it] = to.v[it] = u32x4{0, 0, 0, 0};
+            if (there(id, j)) {
+                const int64_t base = first_row(id, j) * row_bytes;
+                const int off = (r0 % 16 + r_lane) * row_bytes + (in_row ? ch * 16 : 0);
+                to.k[it] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.k) + base + off);
+                to.v[it] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.v) + base + off);
+            }
+        }
+        if constexpr (E8) {
+            // a scale a lane: of keys in one wave (half), of values in another
+            const bool values = SHARED ? wave == 1 : half == 1;
+            to.scale = 0.f;
+            if ((!SHARED || wave < 2) && there(pg.scale, j0 + s_key)) to.scale = (values ? c.v_scale : c.k_scale)[first_row(pg.scale, j0 + s_key)];
+        }
+    };
+    auto keep = [&](Tile& t, int j0, uint16_t* to) INLINE {
+        uint16_t *kk = to, *vv = to + KT * KS;
+        const bool ends = j0 + KT > len;
+#pragma unroll
+        for (int it = 0; it < ITS; ++it) {
+            const int r = row_of(it) + r_lane;
+            const bool out = !in_row || (ends && j0 + r >= len);
+            const u32x4 zero = {0, 0, 0, 0}, x = out ? zero : t.k[it], y = out ? zero : t.v[it];
+            if constexpr (E8) {
+                u32x4 w[2], z[2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[i / 2][i % 2 * 2] = from_e4m3<QBF, false>(x[i]), w[i / 2][i % 2 * 2 + 1] = from_e4m3<QBF, true>(x[i]);
+                    z[i / 2][i % 2 * 2] = from_e4m3<PBF, false>(y[i]), z[i / 2][i % 2 * 2 + 1] = from_e4m3<PBF, true>(y[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    *reinterpret_cast<u32x4*>(kk + r * KS + ch * 16 + 8 * i) = w[i];
+                    *reinterpret_cast<u32x4*>(vv + r * VS + ch * 16 + 8 * i) = z[i];
+                }
+            } else {
+                *reinterpret_cast<u32x4*>(kk + r * KS + ch * 8) = x;
+                *reinterpret_cast<u32x4*>(vv + r * VS + ch * 8) = y;
+            }
+        }
+        if constexpr (E8) {
+            float* scales = reinterpret_cast<float*>(to + KT * (KS + VS));
+            if (SHARED) {
+                if (wave < 2 && lane < KT) scales[wave * KT + lane] = t.scale;
+            } else {
+                scales[lane] = t.scale;
+            }
+        }
+    };
+
+    f32x16 o[DP / 32];
+    float m, l;                                                 // the maximum less OFF, the lane's share of the sum
+    auto clear = [&]() INLINE {
+        m = LOWEST, l = 0.f;
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+    };
+    // The tile of keys j0 on, at `from` in LDS, into o, m and l.
+    // CAREFUL: right for infinite and NaN values, which a weight of 0 makes NaN, and
+    // near the end of float32's range, where weights must not pass 1.
+    auto add_tile = [&](auto care, int j0, const Pages& pg, const uint16_t* from) INLINE {
+        constexpr bool CAREFUL = decltype(care)::value;
+        const uint16_t *kk = from, *vv = from + KT * KS;
+        const float* scales = reinterpret_cast<const float*>(from + KT * (KS + VS));
+        if (j0 + KT <= lo_a || j0 >= hi_z) return;              // nothing that these rows see
+        f32x16 s[KT / 32];
+#pragma unroll
+        for (int b = 0; b < KT / 32; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+            for (int x = 0; x < DP / 16; ++x) {
+                const u32x4 key = *reinterpret_cast<const u32x4*>(kk + (b * 32 + col) * KS + x * 16 + 8 * half);
+                s[b] = mfma32<QBF>(key, q[x], s[b]);
+            }
+        }
+        // scores in units of log2: s times f
+        bool whole = j0 >= lo_z && j0 + KT <= hi_a;
+#pragma unroll
+        for (int g = 0; g < G; ++g) whole = whole && there(pg.id[g], j0 + 16 * g);
+        float f = sc;
+        if (E8 || a.cap > 0.f || a.slopes || !whole) {
+            f = 1.f;
+#pragma unroll
+            for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    f32x4 y = {sc, sc, sc, sc};
+                    if constexpr (E8) y *= *reinterpret_cast<const f32x4*>(scales + b * 32 + 2 * i + 4 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][i + e] *= y[e];
+                }
+            if (a.cap > 0.f) {
+                const float by = p.to_cap, cap = a.cap * LOG2E; // s by = x, tanh(x) cap
+                float top = 0.f;
+#pragma unroll
+                for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[b][i] *= by;
+                        top = __builtin_fmaxf(top, __builtin_fabsf(s[b][i]));
+                    }
+                // where none of the wave's is far, without the exponentials (and more exactly)
+                if (!__any(!(top <= NEAR))) {
+#pragma unroll
+                    for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[b][i] *= cap * tanh_over_x(s[b][i] * s[b][i]);
+                } else {
+#pragma unroll
+                    for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float x = s[b][i], z = __builtin_fabsf(x);
+                            const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * LOG2E * z));
+                            s[b][i] = cap * (z <= NEAR ? x * tanh_over_x(x * x) : __builtin_copysignf(far, x));
+                        }
+                }
+            }
+            if (a.slopes) {
+                const float away = (float)(at - j0 - 4 * half); // of the lane's first key; exact where the product matters
+#pragma unroll
+                for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        s[b][i] = __builtin_fmaf(-slope, __builtin_fabsf(away - (float)(b * 32 + i / 4 * 8 + i % 4)), s[b][i]);
+            }
+            if (!whole) {
+#pragma unroll
+                for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int j = j0 + b * 32 + i / 4 * 8 + i % 4 + 4 * half;
+                        const bool seen = j >= lo && j < hi && there(pg.id[b * 2 + i / 8], j);
+                        s[b][i] = seen ? s[b][i] : -INFINITY;
+                    }
+            }
+        }
+        // the running maximum
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, s[b][i]);
+        top = top * f - OFF;
+        if (__any(top > m + (CAREFUL ? 0.f : SLACK))) {
+            const float y = both_halves_max(__builtin_fmaxf(m, top)), by = __builtin_amdgcn_exp2f(m - y);
+            m = y;
+            l *= by;
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b) o[b] *= by;
+        }
+        // weights
+#pragma unroll
+        for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], f, -m));
+                l += w;
+                s[b][i] = CAREFUL && s[b][i] == -INFINITY ? -1.f : w;   // (careful: none, told from 0)
+            }
+        u32x4 hi8[KT / 16], lo8[TWO ? KT / 16 : 1], any8[CAREFUL ? KT / 16 : 1];
+#pragma unroll
+        for (int x = 0; x < KT / 16; ++x) {
+            f32x4 y[2] = {{1.f, 1.f, 1.f, 1.f}, {1.f, 1.f, 1.f, 1.f}};
+            if constexpr (E8) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) y[i] = *reinterpret_cast<const f32x4*>(scales + KT + x * 16 + 8 * i + 4 * half);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float w0 = s[x / 2][x % 2 * 8 + 2 * i], w1 = s[x / 2][x % 2 * 8 + 2 * i + 1];
+                if constexpr (CAREFUL) {
+                    any8[x][i] = pack<PBF>(w0 < 0.f ? 0.f : 1.f, w1 < 0.f ? 0.f : 1.f);
+                    w0 = w0 < 0.f ? 0.f : E8 ? w0 * y[i / 2][i % 2 * 2] : w0;
+                    w1 = w1 < 0.f ? 0.f : E8 ? w1 * y[i / 2][i % 2 * 2 + 1] : w1;
+                } else if constexpr (E8) {
+                    w0 *= y[i / 2][i % 2 * 2], w1 *= y[i / 2][i % 2 * 2 + 1];
+                }
+                hi8[x][i] = pack<PBF>(w0, w1);
+                if constexpr (TWO) {
+                    const f32x2 z = unpack<PBF>(hi8[x][i]);
+                    lo8[x][i] = pack<PBF>(w0 - z.x, w1 - z.y);
+                    if constexpr (CAREFUL) lo8[x][i] &= ~not_finite<PBF>(hi8[x][i]);
+                }
+            }
+        }
+        // values: columns of the keys whose weights the lane has
+        const uint16_t* column = vv + (4 * half + (lane & 15) / 4) * VS + (lane >> 4 & 1) * 16 + lane % 4 * 4;
+#pragma unroll
+        for (int x = 0; x < KT / 16; ++x)
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b) {
+                const uint2 y = read_columns(column + x * 16 * VS + b * 32), z = read_columns(column + (x * 16 + 8) * VS + b * 32);
+                u32x4 v = {y.x, y.y, z.x, z.y};
+                if constexpr (CAREFUL) {
+                    // infinite and NaN values by kind, where a weight is for them; else 0 in their place
+                    u32x4 out;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) out[i] = v[i] & not_finite<PBF>(v[i]), v[i] &= ~not_finite<PBF>(v[i]);
+#pragma unroll 1
+                    for (int kind = 0; kind < 3; ++kind) {
+                        u32x4 is;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) is[i] = is_kind<PBF>(out[i], kind);
+                        f32x16 n = {};
+                        n = mfma32<PBF>(is, any8[x], n);
+                        const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[b][i] += n[i] > 0.f ? what : 0.f;
+                    }
+                }
+                o[b] = mfma32<PBF>(v, hi8[x], o[b]);
+                if constexpr (TWO) o[b] = mfma32<PBF>(v, lo8[x], o[b]);
+            }
+    };
+    auto not_finite_out = [&]() INLINE {
+        float z = 0.f;
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[b][i], 0.f, z);
+        return z != 0.f;
+    };
+    // LDS that only this wave writes and reads needs no barrier, but the order kept
+    auto settle = [&]() INLINE {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+
+    const int t0 = keys.tile0 + (int)((int64_t)keys.tiles * part / keys.parts);
+    const int t1 = keys.tile0 + (int)((int64_t)keys.tiles * (part + 1) / keys.parts);
+    clear();
+    Tile next;
+    if constexpr (SHARED) {
+        Pages pg{}, pn{};
+        if (t0 < t1) {
+            pg = find(t0 * KT);
+            load(next, t0 * KT, pg);
+            if (t0 + 1 < t1) pn = find((t0 + 1) * KT);
+            keep(next, t0 * KT, lds);
+        }
+        uint16_t *here = lds, *other = lds + BUF;
+        for (int t = t0; t < t1; ++t) {
+            __syncthreads();
+            if (t + 1 < t1) load(next, (t + 1) * KT, pn);
+            Pages pf{};
+            if (t + 2 < t1) pf = find((t + 2) * KT);
+            if (busy) add_tile(std::false_type{}, t * KT, pg, here);
+            if (t + 1 < t1) keep(next, (t + 1) * KT, other);
+            uint16_t* const x = here;
+            here = other, other = x;
+            pg = pn, pn = pf;
+        }
+        if (__builtin_expect(__syncthreads_or(not_finite_out()), 0)) {
+            clear();
+            for (int t = t0; t < t1; ++t) {
+                pg = find(t * KT);
+                load(next, t * KT, pg);
+                __syncthreads();
+                keep(next, t * KT, lds);
+                __syncthreads();
+                if (busy) add_tile(std::true_type{}, t * KT, pg, lds);
+            }
+        }
+    } else {
+        uint16_t* const mine = lds + wave * BUF;
+        int t = t0 + wave;
+        Pages pg{}, pn{};
+        if (t < t1) {
+            pg = find(t * KT);
+            load(next, t * KT, pg);
+            if (t + KW < t1) pn = find((t + KW) * KT);
+        }
+        for (; t < t1; t += KW) {
+            settle();
+            keep(next, t * KT, mine);
+            settle();
+            if (t + KW < t1) load(next, (t + KW) * KT, pn);
+            Pages pf{};
+            if (t + 2 * KW < t1) pf = find((t + 2 * KW) * KT);
+            add_tile(std::false_type{}, t * KT, pg, mine);
+            pg = pn, pn = pf;
+        }
+        if (__builtin_expect(__any(not_finite_out()), 0)) {
+            clear();
+            for (t = t0 + wave; t < t1; t += KW) {
+                pg = find(t * KT);
+                load(next, t * KT, pg);
+                settle();
+                keep(next, t * KT, mine);
+                settle();
+                add_tile(std::true_type{}, t * KT, pg, mine);
+            }
+        }
+    }
+
+    // results: the rows' own, or their part of them
+    const int64_t slot = prompt_slot(p, c.heads, k, head, part);
+    float* const sums = static_cast<float*>(a.ws);
+    float* const stats = sums + prompt_slots(p, c.heads) * DP;
+    l = both_halves_sum(l);
+    if constexpr (SHARED) {
+        const bool store = row0 + col < all;
+        if (keys.parts > 1) {
+            float* const to = sums + (slot + wave * 32 + col) * DP + 4 * half;
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    if (store) *reinterpret_cast<f32x4*>(to + b * 32 + 2 * i) = f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+            if (store && half == 0) {
+                stats[(slot + wave * 32 + col) * 2] = m;
+                stats[(slot + wave * 32 + col) * 2 + 1] = l;
+            }
+            return;
+        }
+        const float f = l == 0.f ? 0.f : 1.0f / l;
+        T* const to = static_cast<T*>(a.out) + (u.first + token) * a.out_row + qh * a.out_head + 4 * half;
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[b][i + e] * f;
+                if (store && b * 32 + 2 * i < c.d) store_values<DT, 4>(to + b * 32 + 2 * i, v);
+            }
+        if (a.lse && store && half == 0)
+            a.lse[(int64_t)(u.first + token) * a.q_heads + qh] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    } else {
+        // the waves' results into one
+        float* const part_o = reinterpret_cast<float*>(lds);
+        float* const part_m = part_o + KW * 32 * (DP + 4);
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4*>(part_o + (wave * 32 + col) * (DP + 4) + b * 32 + 2 * i + 4 * half) =
+                    f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+        if (half == 0) part_m[(wave * 32 + col) * 2] = m, part_m[(wave * 32 + col) * 2 + 1] = l;
+        __syncthreads();
+        constexpr int PER = 64 * KW / 32, OWN = DP / PER;       // threads of a row, elements of a thread
+        const int r = threadIdx.x / PER, d0 = threadIdx.x % PER * OWN, mine = u.tile * M + r;
+        float top = LOWEST, sum = 0.f, v[OWN] = {};
+#pragma unroll
+        for (int w = 0; w < KW; ++w) top = __builtin_fmaxf(top, part_m[(w * 32 + r) * 2]);
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+            const float f = __builtin_amdgcn_exp2f(part_m[(w * 32 + r) * 2] - top);
+            sum = __builtin_fmaf(f, part_m[(w * 32 + r) * 2 + 1], sum);
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) v[i] = __builtin_fmaf(f, part_o[(w * 32 + r) * (DP + 4) + d0 + i], v[i]);
+        }
+        if (mine >= all) return;
+        if (keys.parts > 1) {
+#pragma unroll
+            for (int i = 0; i < OWN; i += 4)
+                *reinterpret_cast<f32x4*>(sums + (slot + r) * DP + d0 + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+            if (d0 == 0) stats[(slot + r) * 2] = top, stats[(slot + r) * 2 + 1] = sum;
+            return;
+        }
+        const float f = sum == 0.f ? 0.f : 1.0f / sum;
+        const int tok = mine / group, h = head * group + mine % group;
+        T* const to = static_cast<T*>(a.out) + (u.first + tok) * a.out_row + h * a.out_head + d0;
+        constexpr int ST = OWN < 16 ? OWN : 16;                 // d is a multiple of 16
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
+#pragma unroll
+        for (int i = 0; i < OWN; i += ST)
+            if (d0 + i < c.d) store_values<DT, ST>(to + i, v + i);
+        if (a.lse && d0 == 0)
+            a.lse[(int64_t)(u.first + tok) * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+    }
+}
+
+template <int DT, int CDT, int DP>
+hipError_t launch_prompt_d(const apc_kv& c, const PromptArgs& a, const PromptPlan& p, hipStream_t s)
+{
+    const dim3 grid((unsigned)((int64_t)p.tiles * c.heads * p.splits));
+    if (p.rows == 32) k_attend_prompt<DT, CDT, DP, 1, 4><<<grid, dim3(256), 0, s>>>(c, a, p);
+    else k_attend_prompt<DT, CDT, DP, 4, 1><<<grid, dim3(256), 0, s>>>(c, a, p);
+    return hipGetLastError();
+}
+
+template <int DT, int CDT>
+hipError_t launch_prompt(const apc_kv& c, const PromptArgs& a, const PromptPlan& p, hipStream_t s)
+{
+    switch (p.dp) {
+    case 64: return launch_prompt_d<DT, CDT, 64>(c, a, p, s);
+    case 128: return launch_prompt_d<DT, CDT, 128>(c, a, p, s);
+    default: return launch_prompt_d<DT, CDT, 256>(c, a, p, s);
+    }
+}
+
+}  // namespace apc

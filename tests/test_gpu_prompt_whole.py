@@ -1,0 +1,553 @@
+"""GPU parity of the operators that read whole prompts against the float64 oracle.
+
+Tolerances, u = 2^-24 (a float32 operation's rounding), half(t) a type's half
+step relative to a value (f16 2^-11, bf16 2^-8):
+* rotation: the angle is within 2^-52 of its size and, reduced, rounded once to
+  float32 turns (at most 1/2, so 2^-25 of a turn: 2^-22.3 radians); sine and cosine
+  within 2 units in the last place, each of the two products and mag within u:
+  2^-21 (|x_a| + |x_b|) |mag| in all, then one rounding to the output's type.
+* attention: a score's error is at most e = (d + 24) u top (top = scale * sum
+  |q k|: a d-term sum, the scales, the exponent's argument), with a cap 2^-21 cap
+  more (the tanh: 2^-22 of the value near 0, at most 2^-21 elsewhere), with
+  slopes 4 u slope |p - j|; so weights are off by a factor of at most 1 + 2 e and
+  the output by 4 e spread; its sums and the sum of weights by 2 (n + 64) u
+  spread (n tokens).  The weights' rounding: half(t) of each where one part
+  carries them, 2^-16 in two parts (f16 in two: 2^-22, taken as 2^-16 too), and
+  over f16 caches at most 2^-37 of the row's heaviest however light.  Then one
+  rounding to the output's type.  lse: 2 e + (n + 64) u + 2^-20 |lse|.
+"""
+import numpy as np
+import pytest
+import torch
+
+from tests.gpu_check import say
+from tests.test_gpu_prompt_ops import KINDS, ROUND, TINY, TORCH, U, f64, gen, make_pool, stored
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def apc():
+    import paper_2502_06798_amd as apc
+    apc.load()
+    assert torch.cuda.is_available()
+    return apc
+
+
+# ---- rotation ----------------------------------------------------------------
+
+def check_rotate(orc, x, at, freq, interleaved, mag, got, dtype, before=None):
+    n = len(freq)
+    want = orc.rotate(x, at, freq, interleaved, mag)
+    a = np.abs(x)
+    tol = np.zeros_like(a)
+    i, j = (np.arange(n) * 2, np.arange(n) * 2 + 1) if interleaved else (np.arange(n), np.arange(n) + n)
+    tol[..., i] = tol[..., j] = 2.0 ** -21 * abs(mag) * (a[..., i] + a[..., j])
+    tol += np.abs(want) * ROUND[dtype] * 1.001 + TINY[dtype]
+    tol[..., 2 * n:] = 0
+    skip = np.asarray(at) < 0
+    if before is not None:
+        want[skip] = before[skip]
+    tol[skip] = 0
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:4], np.abs(got - want)[bad].max())
+
+
+ROTATE = [(1, 1, 2, 2), (3, 2, 64, 64), (1, 16, 64, 64), (257, 3, 80, 40), (100, 5, 128, 128), (33, 40, 128, 64),
+          (77, 7, 96, 30), (5, 1, 256, 256), (9, 4, 255, 254), (13, 3, 66, 34), (2, 61, 128, 30), (40, 2, 17, 10),
+          (1001, 9, 64, 48)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotate_shapes(apc, orc, dtype, interleaved):
+    for t, heads, d, rot in ROTATE:
+        for inplace in (False, True):
+            say(f"rotate {dtype} interleaved={interleaved} t={t} heads={heads} d={d} rot={rot} inplace={inplace}")
+            g = gen(t + d + rot)
+            x = torch.randn((t, heads, d), device="cuda", generator=g).to(TORCH[dtype])
+            at = torch.randint(0, 5000, (t,), device="cuda", generator=g, dtype=torch.int32)
+            at[::5] = -1 - at[::5]
+            freq = torch.from_numpy(apc.apc_rotary_freqs(rot, 10000.0, 4.0, 2048.0)).cuda()
+            r = apc.Rotary(freq, interleaved, 1.25)
+            was = x.clone()
+            out = x if inplace else torch.full_like(x, 7.0)
+            before = f64(out).copy()
+            apc.apc_rotate(r, x, at, out)
+            torch.cuda.synchronize()
+            check_rotate(orc, f64(was), at.cpu().numpy(), freq.cpu().numpy(), interleaved, 1.25, f64(out), dtype, before)
+
+
+def test_rotate_far_positions(apc, orc):
+    """Angles hold at positions where float32 has none left."""
+    at = torch.tensor([0, 1, 2 ** 20, 2 ** 24 + 1, 10 ** 9 + 7, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    x = torch.randn((6, 2, 64), device="cuda", generator=gen(1))
+    freq = torch.from_numpy(apc.apc_rotary_freqs(64)).cuda()
+    out = torch.empty_like(x)
+    apc.apc_rotate(apc.Rotary(freq), x, at, out)
+    torch.cuda.synchronize()
+    # 2^-51 of 2^31 radians is 2^-20: the oracle's product and the kernel's each round once or twice
+    want = orc.rotate(f64(x), at.cpu().numpy(), freq.cpu().numpy(), False)
+    big = np.abs(f64(x))
+    tol = (2.0 ** -21 + at.cpu().numpy()[:, None, None] * 2.0 ** -51) * (big[..., :32] + big[..., 32:])
+    assert (np.abs(f64(out) - want) <= np.concatenate([tol, tol], -1) + np.abs(want) * 2.0 ** -23).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_rotate_views(apc, orc, dtype):
+    """Queries and keys inside a wider row, head-major tensors, any element as the first; what lies between stays."""
+    g = gen(5)
+    t, heads, other, d = 19, 6, 3, 80
+    wide = torch.randn((t, heads + other, d + 5), device="cuda", generator=g).to(TORCH[dtype])
+    was = wide.clone()
+    at = torch.randint(0, 99999, (t,), device="cuda", generator=g, dtype=torch.int32)
+    freq = torch.from_numpy(apc.apc_rotary_freqs(52)).cuda()
+    view = wide[:, 1:1 + heads, 3:3 + d]
+    major = torch.full((heads, t, d), 5.0, device="cuda").to(TORCH[dtype])
+    apc.apc_rotate(apc.Rotary(freq, True), view, at, major.transpose(0, 1))
+    apc.apc_rotate(apc.Rotary(freq), view, at, view)
+    torch.cuda.synchronize()
+    x, p, f = f64(was[:, 1:1 + heads, 3:3 + d]), at.cpu().numpy(), freq.cpu().numpy()
+    check_rotate(orc, x, p, f, True, 1.0, f64(major.transpose(0, 1)), dtype)
+    check_rotate(orc, x, p, f, False, 1.0, f64(view), dtype)
+    rest = torch.ones_like(wide, dtype=torch.bool)
+    rest[:, 1:1 + heads, 3:3 + d] = False
+    assert torch.equal(wide[rest], was[rest])
+    # one token of an expanded tensor, and back by the opposite frequencies
+    y = torch.empty((1, heads, d), device="cuda")
+    z = torch.empty_like(y)
+    x = torch.randn((1, 1, d), device="cuda", generator=g).expand(1, heads, d)
+    apc.apc_rotate(apc.Rotary(freq), x, at[:1], y)
+    apc.apc_rotate(apc.Rotary(-freq), y, at[:1], z)
+    torch.cuda.synchronize()
+    assert (z - x).abs().max() < 1e-5
+
+
+def test_rotate_large(apc):
+    """More threads than one launch of the grid holds heads for: every row is turned as in a small call."""
+    t, heads, d = 40_000, 33, 128
+    x = torch.randn((t, heads, d), device="cuda", generator=gen(6)).to(torch.bfloat16)
+    at = torch.randint(0, 1 << 20, (t,), device="cuda", generator=gen(7), dtype=torch.int32)
+    r = apc.Rotary(torch.from_numpy(apc.apc_rotary_freqs(128)).cuda())
+    out, part = torch.empty_like(x), torch.empty_like(x[:500])
+    apc.apc_rotate(r, x, at, out)
+    for i0 in (0, 20_000, 39_500):
+        apc.apc_rotate(r, x[i0:i0 + 500], at[i0:i0 + 500], part)
+        torch.cuda.synchronize()
+        assert torch.equal(part.view(torch.int16), out[i0:i0 + 500].view(torch.int16))
+
+
+# ---- attention -----------------------------------------------------------------
+
+def make_prompt(seed, sizes, heads, group, d, page, max_pages, cache, dtype, spread=1.0, pad=0):
+    """Sequences of (new, all) tokens: pool, tables, queries (pad rows behind the last sequence), starts, lengths."""
+    g, b = gen(seed), len(sizes)
+    n_pages = b * max_pages + 2
+    kp, vp, ks, vs = make_pool(n_pages, heads, page, d, cache)
+    for p, s in ((kp, ks), (vp, vs)):
+        if s is None:
+            p.copy_(torch.randn(p.shape, device="cuda", generator=g))
+        else:
+            p.copy_(torch.randint(-448, 449, p.shape, device="cuda", generator=g).float())
+            s.copy_(torch.exp(torch.randn(s.shape, device="cuda", generator=g)) / 300)
+    table = torch.randperm(n_pages, device="cuda", generator=g)[:b * max_pages].to(torch.int32).reshape(b, max_pages)
+    new = torch.tensor([n for n, _ in sizes])
+    t = int(new.sum()) + pad
+    starts = torch.cat([new.new_zeros(1), new.cumsum(0)]).to(torch.int32).cuda()
+    lens = torch.tensor([n for _, n in sizes], dtype=torch.int32, device="cuda")
+    q = (torch.randn((t, heads * group, d), device="cuda", generator=g) * spread).to(TORCH[dtype])
+    return (kp, vp, ks, vs), table, q, starts, lens
+
+
+def run_prompt(apc, pool, table, q, starts, lens, scale, stream=None, **kw):
+    c = apc.KvCache(*pool)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    ws = apc.attend_prompt_workspace_tensor(c, q.shape[0], table.shape[0], q.shape[1], table.shape[1])
+    ws.fill_(0xff)                                           # nothing in it needs to start at zero
+    apc.apc_attend_prompt(c, q, starts, table, lens, scale, out, ws, lse, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def check_prompt(orc, cache, dtype, pool, table, q, starts, lens, scale, out, lse, window=0, cap=0.0, slopes=None, prefix=None):
+    k, v, ks, vs = pool
+    host = lambda t: None if t is None else t.cpu().numpy()
+    t, hq, d = q.shape
+    n = table.shape[1] * k.shape[2]
+    with np.errstate(invalid="ignore", over="ignore"):
+        ro, rl, spread, top, heavy, away = orc.attend_prompt(cache, f64(q), host(starts), stored(k), stored(v), host(ks),
+                                                             host(vs), host(table), host(lens), scale, window, cap,
+                                                             host(slopes), host(prefix))
+    e = (d + 24) * U * top + cap * 2.0 ** -21
+    if slopes is not None:
+        e = e + 4 * U * np.abs(host(slopes)).astype(np.float64) * away
+    few = t * (hq // k.shape[1]) <= 32 * min(t, len(lens))
+    weight = 2.0 ** -16 if few or (cache == "e4m3" and dtype == "f16") else ROUND[dtype]
+    got, gl = f64(out), f64(lse)
+    tol = spread * (4 * e + 2 * (n + 64) * U + weight)[..., None] + np.abs(ro) * ROUND[dtype] * 1.001 + TINY[dtype]
+    if cache == "f16":
+        tol = tol + n * 2.0 ** -37 * heavy
+    none = np.isnan(rl)                                      # rows of no sequence
+    assert (got[none] == 7).all() and (gl[none] == 7).all()
+    bad = ~(np.abs(got - ro) <= tol) & ~none[..., None]
+    assert not bad.any(), (np.argwhere(bad)[:4], bad.sum(), np.abs(got - ro)[bad].max())
+    empty = np.isneginf(rl)
+    assert np.array_equal(np.isneginf(gl), empty)
+    assert (got[empty] == 0).all()
+    some = ~none & ~empty
+    assert (np.abs(gl - rl)[some] <= (2 * e + (n + 64) * U + 2.0 ** -20 * np.abs(rl))[some]).all()
+
+
+SIZES = [(1, 1), (2, 40), (0, 10), (33, 33), (17, 100), (0, 0), (129, 130), (65, 200), (1, 200), (31, 31), (64, 64)]
+FEW = [(1, 1), (1, 2), (3, 31), (0, 7), (2, 32), (1, 33), (4, 64), (1, 65), (2, 127), (1, 128), (1, 129), (0, 0), (1, 200)]
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("heads,group,d,page", [(1, 1, 16, 16), (2, 4, 64, 16), (3, 1, 48, 32), (2, 5, 80, 16), (1, 8, 128, 64),
+                                                (2, 3, 128, 16), (1, 16, 128, 128), (8, 1, 64, 256), (2, 2, 96, 256),
+                                                (1, 4, 176, 16), (1, 7, 256, 16), (1, 2, 32, 1024), (2, 1, 208, 32)])
+def test_prompt_lengths(apc, orc, cache, dtype, heads, group, d, page):
+    """Every way new tokens and lengths can end in a row tile, a key tile and a page, with sequences of none among them."""
+    for sizes in (SIZES, FEW):
+        say(f"prompt {dtype} over {cache} heads={heads} group={group} d={d} page={page} n={len(sizes)}")
+        made = make_prompt(d + page, sizes, heads, group, d, page, -(-200 // page), cache, dtype, pad=3)
+        scale = d ** -0.5
+        check_prompt(orc, cache, dtype, *made, scale, *run_prompt(apc, *made, scale))
+
+
+RULES = [dict(window=1), dict(window=16), dict(window=70), dict(cap=2.0), dict(cap=30.0), dict(slopes=0.05), dict(prefix=40),
+         dict(prefix=1000), dict(prefix=90, window=33), dict(cap=1.5, slopes=0.2, window=50, prefix=60),
+         dict(cap=20.0, slopes=1.0), dict(slopes=-0.02, prefix=1000), dict(window=2 ** 31 - 1), dict(prefix=-5),
+         dict(prefix=2 ** 31 - 1, window=2 ** 30)]
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("rule", RULES, ids=[" ".join(f"{k}={v}" for k, v in r.items()) for r in RULES])
+def test_prompt_rules(apc, orc, cache, dtype, rule):
+    """Windows, caps, slopes and prefixes, alone and together."""
+    for d, sizes in ((64, SIZES), (64, FEW), (160, SIZES), (128, FEW), (128, SIZES)):
+        say(f"prompt {rule} {dtype} over {cache} d={d} n={len(sizes)}")
+        made = make_prompt(d, sizes, 2, 3, d, 16, 13, cache, dtype, 2.0)
+        kw = dict(rule)
+        if "slopes" in kw:
+            kw["slopes"] = kw["slopes"] * torch.arange(1, 7, device="cuda", dtype=torch.float32) / 3
+        if "prefix" in kw:
+            kw["prefix"] = torch.full((len(sizes),), kw["prefix"], dtype=torch.int32, device="cuda")
+            kw["prefix"][1] = 3
+        check_prompt(orc, cache, dtype, *made, d ** -0.5, *run_prompt(apc, *made, d ** -0.5, **kw), **kw)
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_prompt_long_keys(apc, orc, cache, dtype, d):
+    """Keys cut into parts: single tokens and pieces over long pasts, beside short and empty sequences."""
+    for sizes in ([(1, 5000), (1, 513), (2, 3000), (0, 100), (1, 1)], [(70, 4000), (150, 2100), (1, 3999), (40, 40)]):
+        for kw in (dict(), dict(window=1500, slopes=torch.full((4,), 0.01, device="cuda"))):
+            say(f"prompt long {dtype} over {cache} d={d} {len(sizes)} {list(kw)}")
+            made = make_prompt(d, sizes, 2, 2, d, 64, 80, cache, dtype, 1.5)
+            check_prompt(orc, cache, dtype, *made, d ** -0.5, *run_prompt(apc, *made, d ** -0.5, **kw), **kw)
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+def test_prompt_few_are_attend(apc, cache, dtype):
+    """Single tokens: what apc_attend says, within the parts' order."""
+    made = make_prompt(3, [(1, n) for n in (1, 50, 700, 2049)], 2, 4, 128, 32, 65, cache, dtype)
+    pool, table, q, starts, lens = made
+    out, lse = run_prompt(apc, *made, 0.1)
+    c, o2, l2 = apc.KvCache(*pool), torch.empty_like(q), torch.empty_like(lse)
+    apc.apc_attend(c, q, table, lens, 0.1, o2, apc.attend_workspace_tensor(c, 4, 8, 65), l2)
+    torch.cuda.synchronize()
+    assert (out.float() - o2.float()).abs().max() <= 2 * ROUND[dtype] * o2.float().abs().max()
+    assert (lse - l2).abs().max() < 1e-4
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+def test_prompt_absent_pages_and_odd_tables(apc, orc, cache, dtype):
+    """Page entries outside the pool leave their tokens out; lengths below 0 and past the table are cut; sequences with
+    more new tokens than they hold; starts outside the rows are cut and falling ones have no row."""
+    sizes = [(40, 200), (3, 100), (70, 208), (50, 20), (9, 50), (5, 5)]
+    for d in (64, 128):
+        pool, table, q, starts, lens = make_prompt(17, sizes, 2, 3, d, 16, 13, cache, dtype, pad=4)
+        n_pages = pool[0].shape[0]
+        table[0, 0], table[0, 5:7], table[1, 6], table[2, 3:] = -1, n_pages, -2 ** 31, 2 ** 31 - 1
+        table[4, :] = -7
+        lens[2], lens[5] = 5000, -3
+        pre = torch.tensor([0, 5, 300, 10, 9, 2], dtype=torch.int32, device="cuda")
+        for kw in (dict(), dict(prefix=pre), dict(window=30, prefix=pre)):
+            for s in (starts, torch.tensor([-4, 40, 43, 30, 50, 10 ** 6, 0], dtype=torch.int32, device="cuda")):
+                say(f"prompt absent {dtype} over {cache} d={d} {list(kw)}")
+                if s is not starts and "window" in kw:
+                    continue
+                got = run_prompt(apc, pool, table, q, s, lens, 0.2, **kw)
+                if s is not starts:             # rows of several sequences hold any of them: only that nothing else is touched
+                    assert (got[0][181:] == 7).all() or torch.isfinite(got[0].float()).all()
+                    continue
+                check_prompt(orc, cache, dtype, pool, table, q, s, lens, 0.2, *got, **kw)
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("fill", [0xff, 0x7f, 0x7c])
+def test_prompt_unseen_slots_hold_anything(apc, cache, dtype, fill):
+    """NaN, infinities and huge values past the lengths, in pages that no table names, and in tokens that a row does not
+    see although others do: bit for bit the same results."""
+    for sizes in ([(40, 100), (17, 33), (70, 208)], [(2, 100), (1, 33), (3, 208)]):
+        pool, table, q, starts, lens = made = make_prompt(13, sizes, 2, 4, 64, 16, 13, cache, dtype)
+        want = run_prompt(apc, *made, 0.125)
+        page = 16
+        seen = torch.zeros((pool[0].shape[0], page), dtype=torch.bool, device="cuda")
+        for i, (_, n) in enumerate(sizes):
+            for j in range(n):
+                seen[table[i, j // page].item(), j % page] = True
+
+        def spoil(keep):
+            for t in pool:
+                if t is not None:
+                    bad = torch.empty_like(t)
+                    bad.view(torch.uint8).fill_(fill)
+                    m = keep[:, None, :].expand(t.shape[:3])
+                    m = m[..., None].expand(t.shape) if t.dim() == 4 else m
+                    raw = t.view(torch.uint8) if t.element_size() == 1 else t.view(torch.int16 if t.element_size() == 2 else torch.int32)
+                    raw.copy_(torch.where(m, raw, bad.view(raw.dtype)))
+
+        say(f"prompt unseen 0x{fill:x} {dtype} over {cache} past the lengths")
+        spoil(seen)
+        for a, b in zip(want, run_prompt(apc, *made, 0.125)):
+            assert torch.equal(a, b)
+        # the last token of each sequence: its own row alone sees it
+        say(f"prompt unseen 0x{fill:x} {dtype} over {cache} later tokens")
+        for i, (_, n) in enumerate(sizes):
+            seen[table[i, (n - 1) // page].item(), (n - 1) % page] = False
+        spoil(seen)
+        got = run_prompt(apc, *made, 0.125)
+        last = torch.zeros(q.shape[0], dtype=torch.bool, device="cuda")
+        last[(starts[1:] - 1).long()] = True
+        # (a wave that met such values goes over its tiles again with every weight below 1: its sums round otherwise)
+        assert torch.isfinite(got[0][~last].float()).all()
+        d = (got[0][~last].float() - want[0][~last].float()).abs()
+        assert (d <= 4 * ROUND[dtype] * want[0][~last].float().abs() + 4 * ROUND[dtype] * 3.0).all()
+        assert (got[1][~last] - want[1][~last]).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_prompt_infinite_values(apc, orc, dtype, d):
+    """Infinite and NaN values reach the elements that they stand in of the rows that see them, and nothing else."""
+    for sizes in ([(40, 100), (70, 150)], [(2, 100), (3, 150)]):
+        say(f"prompt infinite {dtype} d={d} {sizes}")
+        made = make_prompt(19, sizes, 1, 2, d, 16, 10, dtype, dtype)
+        pool, table, q, starts, lens = made
+        want, wl = run_prompt(apc, *made, d ** -0.5)
+        v = pool[1]
+        put = [(0, 97, 3, float("inf")), (0, 98, 3, float("-inf")), (0, 98, 5, float("-inf")), (1, 149, 7, float("nan")),
+               (1, 20, d - 1, float("inf"))]
+        for i, j, e, x in put:
+            v[table[i, j // 16].item(), 0, j % 16, e] = x
+        got, gl = run_prompt(apc, *made, d ** -0.5)
+        expect = want.float().clone()
+        for i, (n, length) in enumerate(sizes):
+            for r in range(n):
+                p = length - n + r
+                sums = {}
+                for i2, j, e, x in put:
+                    if i2 == i and j <= p:
+                        sums[e] = sums.get(e, 0.0) + x
+                for e, x in sums.items():
+                    expect[int(starts[i]) + r, :, e] = x
+        g = got.float()
+        assert torch.equal(torch.isnan(g), torch.isnan(expect)) and torch.equal(torch.isinf(g), torch.isinf(expect))
+        assert torch.equal(g[torch.isinf(g)], expect[torch.isinf(expect)])
+        fine = torch.isfinite(expect)
+        assert ((g - expect).abs()[fine] <= 4 * ROUND[dtype] * expect.abs()[fine] + 4 * ROUND[dtype] * 3.0).all()
+        assert (gl - wl).abs().max() < 1e-5
+
+
+def test_prompt_values_near_the_end_of_the_range(apc, orc):
+    """bf16 values up to 2^127.9: weighted means stay inside float32 although weights of 2^8 would not."""
+    for sizes in ([(40, 64), (70, 100)], [(2, 64), (3, 100)]):
+        made = make_prompt(23, sizes, 1, 2, 64, 16, 7, "bf16", "bf16", 4.0)
+        made[0][1].copy_((torch.randn(made[0][1].shape, device="cuda", generator=gen(1)).clamp(-2, 2) * 2.0 ** 119))
+        check_prompt(orc, "bf16", "bf16", *made, 0.3, *run_prompt(apc, *made, 0.3))
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+def test_prompt_scores_at_the_ends(apc, cache, dtype):
+    """Keys that score -inf drop out; +inf and NaN scores make their rows NaN, as a float32 softmax does; others stay."""
+    if cache == "e4m3":
+        return                                               # (codes have no infinity)
+    for sizes in ([(40, 60)], [(2, 60)]):
+        pool, table, q, starts, lens = made = make_prompt(29, sizes, 1, 1, 64, 16, 4, cache, dtype)
+        q[:, :, 0] = q[:, :, 0].abs() + 0.5
+        want = run_prompt(apc, *made, 0.125)
+        k = pool[0]
+        at = lambda j: (table[0, j // 16].item(), 0, j % 16)
+        keep = k[at(59)].clone()
+        k[at(59)][0] = float("inf")                          # seen by the last row alone
+        got = run_prompt(apc, *made, 0.125)
+        assert torch.isnan(got[0][-1]).all() and torch.isnan(got[1][-1]).all()
+        assert torch.equal(got[0][:-1], want[0][:-1]) and torch.equal(got[1][:-1], want[1][:-1])
+        k[at(59)] = keep
+        k[at(58)][0] = float("-inf")
+        got = run_prompt(apc, *made, 0.125)
+        assert torch.isfinite(got[0].float()).all() and torch.isfinite(got[1]).all()
+        # every key of the first row
+        q2, s2, l2 = q[:1], torch.tensor([0, 1], dtype=torch.int32, device="cuda"), torch.tensor([1], dtype=torch.int32, device="cuda")
+        k[at(0)][0] = float("-inf")
+        out, lse = run_prompt(apc, pool, table, q2, s2, l2, 0.125)
+        assert not out.any() and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("scale", [0.0, -0.2])
+def test_prompt_scale_signs(apc, orc, cache, dtype, scale):
+    for sizes in (SIZES, FEW):
+        made = make_prompt(31, sizes, 2, 2, 64, 16, 13, cache, dtype)
+        check_prompt(orc, cache, dtype, *made, scale, *run_prompt(apc, *made, scale))
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+def test_prompt_light_weights(apc, orc, cache, dtype):
+    """A heavy token whose value is 0 and many light ones that make the output."""
+    for n in (40, 2):
+        pool, table, q, starts, lens = made = make_prompt(37, [(n, 1000)], 1, 1, 64, 64, 16, cache, dtype)
+        q.zero_()
+        q[:, :, 0] = 1.0
+        pool[0].view(torch.uint8).zero_()
+        heavy = (table[0, 0].item(), 0, 5)
+        pool[0][heavy][0] = 14.0
+        if pool[2] is not None:
+            pool[2].fill_(1.0)
+        pool[1][heavy].view(torch.uint8).zero_()
+        check_prompt(orc, cache, dtype, *made, 1.0, *run_prompt(apc, *made, 1.0))
+
+
+def test_prompt_views(apc, orc):
+    """Queries inside a fused product's rows, head-major outputs, page tables inside wider ones, no lse."""
+    pool, table, q, starts, lens = make_prompt(41, SIZES, 2, 4, 80, 16, 13, "bf16", "bf16", pad=2)
+    want, _ = run_prompt(apc, pool, table, q, starts, lens, 0.1)
+    t = q.shape[0]
+    wide = torch.randn((t, 13, 83), device="cuda").to(torch.bfloat16)
+    wide[:, 2:10, 1:81] = q
+    out = torch.full((8, t, 90), 7.0, device="cuda").to(torch.bfloat16)
+    tables = torch.full((len(SIZES), 29), -9, dtype=torch.int32, device="cuda")
+    tables[:, 3:16] = table
+    c = apc.KvCache(*pool)
+    ws = apc.attend_prompt_workspace_tensor(c, t, len(SIZES), 8, 13)
+    apc.apc_attend_prompt(c, wide[:, 2:10, 1:81], starts, tables[:, 3:16], lens, 0.1, out.transpose(0, 1)[:, :, 5:85], ws)
+    torch.cuda.synchronize()
+    assert torch.equal(out.transpose(0, 1)[:, :, 5:85], want)
+    assert (out[:, :, :5] == 7).all() and (out[:, :, 85:] == 7).all()
+
+
+def test_prompt_many_sequences(apc, orc):
+    """More sequences than a step of the search takes, most of them without a row."""
+    rng = np.random.default_rng(1)
+    sizes = [(int(n), int(n) + int(p)) for n, p in zip(rng.integers(0, 3, 700) * (rng.random(700) < 0.3), rng.integers(0, 12, 700))]
+    sizes[555] = (140, 150)
+    made = make_prompt(43, sizes, 1, 2, 16, 16, 10, "bf16", "bf16")
+    check_prompt(orc, "bf16", "bf16", *made, 0.25, *run_prompt(apc, *made, 0.25))
+
+
+def test_prompt_empty_pool(apc):
+    c = apc.KvCache(*(torch.empty((0, 2, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    q = torch.ones((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.ones_like(q), torch.ones((3, 2), device="cuda")
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    apc.apc_attend_prompt(c, q, i32(0, 3), i32(0, 0).view(1, 2), i32(20), 1.0, out, apc.attend_prompt_workspace_tensor(c, 3, 1, 2, 2), lse)
+    torch.cuda.synchronize()
+    assert not out.any() and torch.isneginf(lse).all()
+
+
+def test_prompt_streams_and_graph(apc):
+    """Calls on two streams with workspaces of their own at once, and both operators captured and replayed with other
+    inputs in the same buffers: the results of calls alone."""
+    sizes = [(1, 3000), (2, 2500), (1, 700)]
+    many = [(200, 2000), (90, 90)]
+    freq = torch.from_numpy(apc.apc_rotary_freqs(64)).cuda()
+    rotary = apc.Rotary(freq)
+    work = []
+    for seed, s in ((1, sizes), (2, many)):
+        pool, table, q, starts, lens = make_prompt(seed, s, 2, 2, 64, 64, 47, "bf16", "bf16")
+        c = apc.KvCache(*pool)
+        ws = apc.attend_prompt_workspace_tensor(c, q.shape[0], len(s), 4, 47)
+        at = torch.arange(q.shape[0], dtype=torch.int32, device="cuda")
+        work.append(dict(c=c, q=q, turned=torch.empty_like(q), at=at, starts=starts, table=table, lens=lens, ws=ws,
+                         out=torch.empty_like(q), lse=torch.empty(q.shape[:2], device="cuda"), pool=pool))
+
+    def go(w, stream=None):
+        apc.apc_rotate(rotary, w["q"], w["at"], w["turned"], stream=stream)
+        apc.apc_attend_prompt(w["c"], w["turned"], w["starts"], w["table"], w["lens"], 0.125, w["out"], w["ws"], w["lse"],
+                              stream=stream)
+
+    alone = []
+    for w in work:
+        go(w)
+        torch.cuda.synchronize()
+        alone.append((w["out"].clone(), w["lse"].clone()))
+    streams = [torch.cuda.Stream() for _ in work]
+    for _ in range(5):
+        for w, s in zip(work, streams):
+            w["out"].fill_(3.0)
+        torch.cuda.synchronize()
+        for w, s in zip(work, streams):
+            go(w, s)
+        torch.cuda.synchronize()
+        for w, (o, l) in zip(work, alone):
+            assert torch.equal(w["out"], o) and torch.equal(w["lse"], l)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for w in work:
+            go(w)
+    for turn in range(4):
+        for w in work:
+            w["q"].copy_(torch.randn(w["q"].shape, device="cuda", generator=gen(turn)))
+            w["out"].fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [(w["out"].clone(), w["lse"].clone()) for w in work]
+        for w, (o, l) in zip(work, got):
+            go(w)
+            torch.cuda.synchronize()
+            assert torch.equal(w["out"], o) and torch.equal(w["lse"], l)
+
+
+def test_prompt_results_do_not_depend_on_the_run(apc):
+    """The same call again: bit for bit, also where keys are cut into parts."""
+    made = make_prompt(47, [(1, 9000), (150, 8000)], 2, 4, 128, 64, 141, "e4m3", "bf16")
+    first = run_prompt(apc, *made, 0.1)
+    for _ in range(3):
+        for a, b in zip(first, run_prompt(apc, *made, 0.1)):
+            assert torch.equal(a, b)
+
+
+def test_prompt_offsets_past_32_bits(apc, orc):
+    """Pages, queries and outputs whose elements lie past 2^31."""
+    page, heads, d = 1024, 8, 256
+    n_pages = 1100                                           # 2.3e9 elements
+    k = torch.zeros((n_pages, heads, page, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    g = gen(3)
+    for p in (0, 1098, 1099):
+        k[p].copy_(torch.randn(k[p].shape, device="cuda", generator=g))
+        v[p].copy_(torch.randn(v[p].shape, device="cuda", generator=g))
+    table = torch.tensor([[1098, 0], [0, 1099]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([1500, 1030], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 3, 40], dtype=torch.int32, device="cuda")
+    row = 60_000_000                                         # 39 rows of it: 2.3e9 elements
+    big = torch.zeros(40 * row, dtype=torch.bfloat16, device="cuda")
+    q = big.as_strided((40, heads, d), (row, d, 1))
+    q.copy_(torch.randn((40, heads, d), device="cuda", generator=g))
+    c = apc.KvCache(k, v)
+    ws = apc.attend_prompt_workspace_tensor(c, 40, 2, heads, 2)
+    out, lse = big.as_strided((40, heads, d), (row, d, 1), heads * d), torch.empty((40, heads), device="cuda")
+    apc.apc_attend_prompt(c, q, starts, table, lens, d ** -0.5, out, ws, lse)
+    torch.cuda.synchronize()
+    small = [torch.stack([x[1098], x[0], x[1099]]) for x in (k, v)]
+    at = torch.tensor([[0, 1], [1, 2]], dtype=torch.int32, device="cuda")
+    check_prompt(orc, "bf16", "bf16", (small[0], small[1], None, None), at, q, starts, lens, d ** -0.5, out, lse)
+    turned = big.as_strided((40, heads, d), (row, d, 1), 2 * heads * d)
+    pos = torch.arange(40, dtype=torch.int32, device="cuda")
+    freq = torch.from_numpy(apc.apc_rotary_freqs(d)).cuda()
+    apc.apc_rotate(apc.Rotary(freq), q, pos, turned)
+    torch.cuda.synchronize()
+    check_rotate(orc, f64(q), pos.cpu().numpy(), freq.cpu().numpy(), False, 1.0, f64(turned), "bf16")
