@@ -26,13 +26,14 @@ COUNTED = ["qs_f16.hip", "qs_bf16.hip", "qs_e4m3.hip", "qs8_f16.hip", "qs8_bf16.
 # compiler adds only make a wait longer.  Its tiles of 256 queries spill a few
 # registers (bytes per lane, the other tiles none); more would cost time.  The
 # attention kernels use none, the norm's those of float32 rows beyond 16,384.
-SCRATCH = {"tile_f32.hip": 0, "tile_f16.hip": 24, "tile_bf16.hip": 24, "tile_e4m3.hip": 12, "attend.hip": 0, "norm.hip": 240}
+SCRATCH = {"tile_f32.hip": 0, "tile_f16.hip": 24, "tile_bf16.hip": 24, "tile_e4m3.hip": 12, "attend.hip": 0, "norm.hip": 240,
+           "prompt_f16.hip": 0, "prompt_bf16.hip": 0, "prompt_e4m3.hip": 0}
 
 # Kernels in these sources keep values of every lane in registers across
 # branches that only some lanes take.  Where registers are short the compiler
 # may move such a value to another place inside the branch, and the other lanes'
 # is lost; so no kernel may write an accumulation register or scratch memory there.
-ALL_LANES = ["attend.hip"]
+ALL_LANES = ["attend.hip", "prompt_f16.hip", "prompt_bf16.hip", "prompt_e4m3.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -96,7 +97,8 @@ def masked_moves(asm: str) -> list:
         if on and after < len(order):
             ways.append((order[after], tuple(saved)))
         for way, masks in ways:
-            if way in blocks and (way not in saved_at or len(saved_at[way]) < len(masks)):
+            # (a loop that saves a mask each time round ends with 64)
+            if way in blocks and (way not in saved_at or len(saved_at[way]) < len(masks) <= 64):
                 saved_at[way] = masks
                 todo.append(way)
     return sorted(found)

@@ -168,6 +168,9 @@ __device__ inline int64_t prompt_slot(const PromptPlan& p, int heads, int k, int
     return (((int64_t)k * heads + head) * p.splits + part) * p.rows;
 }
 
+// Every lane takes part in all of the loop: where registers are short the compiler
+// may move one of the sums to another register inside a branch that only some lanes
+// take, and the other lanes' is lost (heads of 256 over f16: wrong values so).
 template <int DT, int CDT, int DP, int R, int KW>
 __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt(apc_kv c, PromptArgs a, PromptPlan p)
 {
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     // 2^OFF to 2^15, so weights from 2^-26 of it are whole and those below 2^-36 are left out.
     constexpr float SLACK = PBF ? 8.f : 3.f, OFF = PBF ? 0.f : 12.f;
     constexpr int M = 32 * R, ES = E8 ? 1 : 2;
-    constexpr int KT = SHARED && DP <= 128 ? 64 : 32, G = KT / 16;  // keys of a tile, sixteens of them (no page is smaller)
+    constexpr int KT = SHARED && DP <= 128 ? 64 : 32;           // keys of a tile
     constexpr int NT = SHARED ? 64 * R : 64;                    // threads that load a tile
     constexpr int CH = DP * ES / 16, RW = 64 / CH;              // 16-byte pieces of a row, rows of a wave's load
     constexpr int ITS = KT * CH / NT, STEP = NT / CH;           // loads of a thread, rows between them
@@ -237,51 +240,61 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     const int32_t* table = a.pages + u.seq * a.ld_pages;
     const int last_page = (len - 1) >> p.shift;
     const int r_lane = lane / CH, ch = lane % CH;
-    const int s_key = SHARED ? lane % KT : lane & 31;           // whose scale the lane loads
     auto row_of = [&](int it) INLINE { return it * STEP + (SHARED ? wave * RW : 0); };
-    struct Pages { int32_t id[G], own[ITS], scale; };           // of the sixteens, of the thread's rows, of its scale
+    // A tile's page entries: a lane has the one of key lane % KT.  (By a vector load, which is
+    // in order with the others: scalar loads would have the first LDS operand wait for them.)
     auto find = [&](int j0) INLINE {
-        Pages pg;
-        auto index = [&](int j) INLINE { return j >> p.shift < last_page ? j >> p.shift : last_page; };
-#pragma unroll
-        for (int g = 0; g < G; ++g) pg.id[g] = table_entry(table, index(j0 + 16 * g));
-#pragma unroll
-        for (int it = 0; it < ITS; ++it) pg.own[it] = SHARED ? table_entry(table, index(j0 + row_of(it))) : pg.id[it * STEP / 16];
-        pg.scale = E8 ? table[index(j0 + s_key)] : 0;
-        return pg;
+        const int i = (j0 + lane % KT) >> p.shift;
+        return table[i < last_page ? i : last_page];
     };
-    auto there = [&](int32_t id, int j) INLINE { return (uint32_t)id < (uint64_t)c.n_pages && j < len; };
+    auto page_of = [&](int32_t pages, int r) INLINE { return __builtin_amdgcn_readlane(pages, r / 16 * 16); };
+    auto there = [&](int32_t id, int j) INLINE { return ((uint32_t)id < (uint64_t)c.n_pages) & (j < len); };
+    auto all_there = [&](int32_t pages, int j) INLINE { return __all(there(pages, j)); };
     auto first_row = [&](int32_t id, int j) INLINE { return (((int64_t)id * c.heads + head) << p.shift) + (j & in_page); };
     const bool in_row = ch * 16 < row_bytes;
     struct Tile { u32x4 k[ITS], v[ITS]; float scale; };
-    auto load = [&](Tile& to, int j0, const Pages& pg) INLINE {
+    // a lane's place among the sixteen rows that its wave's load is in; past a row's end it reads the row's first piece
+    const uint32_t place = (uint32_t)((row_of(0) % 16 + r_lane) * row_bytes + (in_row ? ch * 16 : 0));
+    auto load = [&](Tile& to, int j0, int32_t pages) INLINE {
+        auto one = [&](int it) INLINE {
+            const int j = j0 + row_of(it) / 16 * 16;
+            const int64_t base = first_row(page_of(pages, row_of(it)), j) * row_bytes;
+            const uint32_t off = place + (uint32_t)(it * STEP % 16 * row_bytes);
+            to.k[it] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.k) + base + off);
+            to.v[it] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.v) + base + off);
+        };
+        if (__builtin_expect(all_there(pages, j0 + lane % KT / 16 * 16), 1)) {
 #pragma unroll
-        for (int it = 0; it < ITS; ++it) {
-            const int r0 = row_of(it), j = j0 + r0 / 16 * 16;
-            const int32_t id = pg.own[it];
-            to.k[it] = to.v[it] = u32x4{0, 0, 0, 0};
-            if (there(id, j)) {
-                const int64_t base = first_row(id, j) * row_bytes;
-                const int off = (r0 % 16 + r_lane) * row_bytes + (in_row ? ch * 16 : 0);
-                to.k[it] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.k) + base + off);
-                to.v[it] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.v) + base + off);
+            for (int it = 0; it < ITS; ++it) one(it);
+        } else {
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) {
+                to.k[it] = to.v[it] = u32x4{0, 0, 0, 0};
+                if (there(page_of(pages, row_of(it)), j0 + row_of(it) / 16 * 16)) one(it);
             }
         }
         if constexpr (E8) {
             // a scale a lane: of keys in one wave (half), of values in another
             const bool values = SHARED ? wave == 1 : half == 1;
             to.scale = 0.f;
-            if ((!SHARED || wave < 2) && there(pg.scale, j0 + s_key)) to.scale = (values ? c.v_scale : c.k_scale)[first_row(pg.scale, j0 + s_key)];
+            const int j = j0 + lane % KT;
+            if ((!SHARED | (wave < 2)) & there(pages, j)) to.scale = (values ? c.v_scale : c.k_scale)[first_row(pages, j)];
         }
     };
     auto keep = [&](Tile& t, int j0, uint16_t* to) INLINE {
         uint16_t *kk = to, *vv = to + KT * KS;
-        const bool ends = j0 + KT > len;
+        if (c.d < DP || j0 + KT > len) {
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) {
+                const bool out = !in_row | (j0 + row_of(it) + r_lane >= len);
+                const u32x4 zero = {0, 0, 0, 0};
+                t.k[it] = out ? zero : t.k[it], t.v[it] = out ? zero : t.v[it];
+            }
+        }
 #pragma unroll
         for (int it = 0; it < ITS; ++it) {
             const int r = row_of(it) + r_lane;
-            const bool out = !in_row || (ends && j0 + r >= len);
-            const u32x4 zero = {0, 0, 0, 0}, x = out ? zero : t.k[it], y = out ? zero : t.v[it];
+            const u32x4 x = t.k[it], y = t.v[it];
             if constexpr (E8) {
                 u32x4 w[2], z[2];
 #pragma unroll
@@ -321,26 +334,43 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     // The tile of keys j0 on, at `from` in LDS, into o, m and l.
     // CAREFUL: right for infinite and NaN values, which a weight of 0 makes NaN, and
     // near the end of float32's range, where weights must not pass 1.
-    auto add_tile = [&](auto care, int j0, const Pages& pg, const uint16_t* from) INLINE {
+    auto add_tile = [&](auto care, int j0, int32_t pages, const uint16_t* from) INLINE {
         constexpr bool CAREFUL = decltype(care)::value;
         const uint16_t *kk = from, *vv = from + KT * KS;
         const float* scales = reinterpret_cast<const float*>(from + KT * (KS + VS));
         if (j0 + KT <= lo_a || j0 >= hi_z) return;              // nothing that these rows see
-        f32x16 s[KT / 32];
+        float s[KT / 32][16];
+        // operands from LDS, AHEAD of them on their way (left to itself the compiler waits for each before its product)
+        constexpr int NK = KT / 32 * (DP / 16), NV = KT / 16 * (DP / 32), AHEAD = 4;
+        auto key_at = [&](int i) INLINE {                       // i: elements 16 (i / (KT / 32)) on of keys 32 (i % (KT / 32)) on
+            return *reinterpret_cast<const u32x4*>(kk + (i % (KT / 32) * 32 + col) * KS + i / (KT / 32) * 16 + 8 * half);
+        };
+        {
+            u32x4 key[AHEAD];
+            f32x16 sum[KT / 32];
 #pragma unroll
-        for (int b = 0; b < KT / 32; ++b) {
+            for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+                for (int i = 0; i < 16; ++i) sum[b][i] = 0.f;
 #pragma unroll
-            for (int x = 0; x < DP / 16; ++x) {
-                const u32x4 key = *reinterpret_cast<const u32x4*>(kk + (b * 32 + col) * KS + x * 16 + 8 * half);
-                s[b] = mfma32<QBF>(key, q[x], s[b]);
+            for (int i = 0; i < AHEAD; ++i) key[i] = key_at(i);
+            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+            for (int i = 0; i < NK; ++i) {
+                sum[i % (KT / 32)] = mfma32<QBF>(key[i % AHEAD], q[i / (KT / 32)], sum[i % (KT / 32)]);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (i + AHEAD < NK) {
+                    key[i % AHEAD] = key_at(i + AHEAD);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
             }
+#pragma unroll
+            for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = sum[b][i];
         }
         // scores in units of log2: s times f
-        bool whole = j0 >= lo_z && j0 + KT <= hi_a;
-#pragma unroll
-        for (int g = 0; g < G; ++g) whole = whole && there(pg.id[g], j0 + 16 * g);
+        const bool whole = j0 >= lo_z && j0 + KT <= hi_a && all_there(pages, j0 + lane % KT);
         float f = sc;
         if (E8 || a.cap > 0.f || a.slopes || !whole) {
             f = 1.f;
@@ -374,14 +404,20 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
                     for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float x = s[b][i], z = __builtin_fabsf(x);
+                            // (told apart from the other branch's, or the compiler computes all of the near
+                            // ones before the branch, and runs out of registers)
+                            float x = s[b][i];
+                            asm volatile("" : "+v"(x));
+                            const float z = __builtin_fabsf(x);
                             const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * LOG2E * z));
-                            s[b][i] = cap * (z <= NEAR ? x * tanh_over_x(x * x) : __builtin_copysignf(far, x));
+                            const float near = x * tanh_over_x(x * x), y = __builtin_copysignf(far, x);
+                            s[b][i] = cap * (z <= NEAR ? near : y);
                         }
                 }
             }
             if (a.slopes) {
-                const float away = (float)(at - j0 - 4 * half); // of the lane's first key; exact where the product matters
+                float away = (float)(at - j0 - 4 * half);       // of the lane's first key; exact where the product matters
+                asm volatile("" : "+v"(away));
 #pragma unroll
                 for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
@@ -389,14 +425,23 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
                         s[b][i] = __builtin_fmaf(-slope, __builtin_fabsf(away - (float)(b * 32 + i / 4 * 8 + i % 4)), s[b][i]);
             }
             if (!whole) {
+                // of the lane's keys, those from `from` to `to` on; sixteens whose page is not there
+                int from = lo - j0 - 4 * half;
+                const int width = hi > lo ? hi - lo : 0;
+                asm volatile("" : "+v"(from));                  // (or the loop would keep every key's distance from `lo`)
 #pragma unroll
                 for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int j = j0 + b * 32 + i / 4 * 8 + i % 4 + 4 * half;
-                        const bool seen = j >= lo && j < hi && there(pg.id[b * 2 + i / 8], j);
-                        s[b][i] = seen ? s[b][i] : -INFINITY;
+                        const uint32_t at = (uint32_t)(b * 32 + i / 4 * 8 + i % 4 - from);
+                        s[b][i] = at < (uint32_t)width ? s[b][i] : -INFINITY;
                     }
+#pragma unroll
+                for (int g = 0; g < KT / 16; ++g) {
+                    if (there(page_of(pages, g * 16), j0 + g * 16)) continue;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[g / 2][g % 2 * 8 + i] = -INFINITY;
+                }
             }
         }
         // the running maximum
@@ -414,14 +459,16 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             for (int b = 0; b < DP / 32; ++b) o[b] *= by;
         }
         // weights
+        float l1 = 0.f;
 #pragma unroll
         for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], f, -m));
-                l += w;
+                (i % 2 ? l1 : l) += w;
                 s[b][i] = CAREFUL && s[b][i] == -INFINITY ? -1.f : w;   // (careful: none, told from 0)
             }
+        l += l1;
         u32x4 hi8[KT / 16], lo8[TWO ? KT / 16 : 1], any8[CAREFUL ? KT / 16 : 1];
 #pragma unroll
         for (int x = 0; x < KT / 16; ++x) {
@@ -450,32 +497,50 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         }
         // values: columns of the keys whose weights the lane has
         const uint16_t* column = vv + (4 * half + (lane & 15) / 4) * VS + (lane >> 4 & 1) * 16 + lane % 4 * 4;
+        auto values_at = [&](int i) INLINE {                    // i: elements 32 (i % (DP / 32)) on of keys 16 (i / (DP / 32)) on
+            const uint16_t* from = column + i / (DP / 32) * 16 * VS + i % (DP / 32) * 32;
+            const uint2 y = read_columns(from), z = read_columns(from + 8 * VS);
+            return u32x4{y.x, y.y, z.x, z.y};
+        };
+        if constexpr (!CAREFUL) {
+            u32x4 v[AHEAD];
 #pragma unroll
-        for (int x = 0; x < KT / 16; ++x)
+            for (int i = 0; i < AHEAD; ++i) v[i] = values_at(i);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
 #pragma unroll
-            for (int b = 0; b < DP / 32; ++b) {
-                const uint2 y = read_columns(column + x * 16 * VS + b * 32), z = read_columns(column + (x * 16 + 8) * VS + b * 32);
-                u32x4 v = {y.x, y.y, z.x, z.y};
-                if constexpr (CAREFUL) {
-                    // infinite and NaN values by kind, where a weight is for them; else 0 in their place
-                    u32x4 out;
+            for (int i = 0; i < NV; ++i) {
+                const int x = i / (DP / 32), b = i % (DP / 32);
+                o[b] = mfma32<PBF>(v[i % AHEAD], hi8[x], o[b]);
+                if constexpr (TWO) o[b] = mfma32<PBF>(v[i % AHEAD], lo8[x], o[b]);
+                __builtin_amdgcn_sched_group_barrier(0x008, TWO ? 2 : 1, 0);
+                if (i + AHEAD < NV) {
+                    v[i % AHEAD] = values_at(i + AHEAD);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                }
+            }
+        } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) out[i] = v[i] & not_finite<PBF>(v[i]), v[i] &= ~not_finite<PBF>(v[i]);
+            for (int i = 0; i < NV; ++i) {
+                // infinite and NaN values by kind, where a weight is for them; else 0 in their place
+                const int x = i / (DP / 32), b = i % (DP / 32);
+                u32x4 v = values_at(i), out;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = v[e] & not_finite<PBF>(v[e]), v[e] &= ~not_finite<PBF>(v[e]);
 #pragma unroll 1
-                    for (int kind = 0; kind < 3; ++kind) {
-                        u32x4 is;
+                for (int kind = 0; kind < 3; ++kind) {
+                    u32x4 is;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) is[i] = is_kind<PBF>(out[i], kind);
-                        f32x16 n = {};
-                        n = mfma32<PBF>(is, any8[x], n);
-                        const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+                    for (int e = 0; e < 4; ++e) is[e] = is_kind<PBF>(out[e], kind);
+                    f32x16 n = {};
+                    n = mfma32<PBF>(is, any8[x], n);
+                    const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[b][i] += n[i] > 0.f ? what : 0.f;
-                    }
+                    for (int e = 0; e < 16; ++e) o[b][e] += n[e] > 0.f ? what : 0.f;
                 }
                 o[b] = mfma32<PBF>(v, hi8[x], o[b]);
                 if constexpr (TWO) o[b] = mfma32<PBF>(v, lo8[x], o[b]);
             }
+        }
     };
     auto not_finite_out = [&]() INLINE {
         float z = 0.f;
@@ -496,7 +561,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     clear();
     Tile next;
     if constexpr (SHARED) {
-        Pages pg{}, pn{};
+        int32_t pg = 0, pn = 0;
         if (t0 < t1) {
             pg = find(t0 * KT);
             load(next, t0 * KT, pg);
@@ -507,7 +572,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         for (int t = t0; t < t1; ++t) {
             __syncthreads();
             if (t + 1 < t1) load(next, (t + 1) * KT, pn);
-            Pages pf{};
+            int32_t pf = 0;
             if (t + 2 < t1) pf = find((t + 2) * KT);
             if (busy) add_tile(std::false_type{}, t * KT, pg, here);
             if (t + 1 < t1) keep(next, (t + 1) * KT, other);
@@ -529,7 +594,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     } else {
         uint16_t* const mine = lds + wave * BUF;
         int t = t0 + wave;
-        Pages pg{}, pn{};
+        int32_t pg = 0, pn = 0;
         if (t < t1) {
             pg = find(t * KT);
             load(next, t * KT, pg);
@@ -540,7 +605,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             keep(next, t * KT, mine);
             settle();
             if (t + KW < t1) load(next, (t + KW) * KT, pn);
-            Pages pf{};
+            int32_t pf = 0;
             if (t + 2 * KW < t1) pf = find((t + 2 * KW) * KT);
             add_tile(std::false_type{}, t * KT, pg, mine);
             pg = pn, pn = pf;
