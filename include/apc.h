@@ -642,7 +642,7 @@ apc_status apc_attend_prompt_workspace(const apc_kv* c /* host */, int64_t t, in
  * lengths     b int32.
  * prefix      b int32, or NULL: no prefix.
  * slopes      q_heads float32, or NULL: no bias.
- * window      >= 0 (0: none).   cap: finite, >= 0 (0: none).   scale: finite.
+ * window      >= 0 (0: none).   cap: finite, >= 0 (0, or above 2^100: none).   scale: finite.
  * lse         t x q_heads float32, or NULL.
  * ws          workspace of at least apc_attend_prompt_workspace() bytes (16-byte
  *             aligned); nothing in it needs to start at zero.

@@ -114,8 +114,9 @@ struct PromptPlan {
     int32_t rows;        // of a row tile: 32 or 128
     int32_t tiles;       // row tiles of a key-value head, at most
     int32_t splits;      // parts of a unit's keys, at most
+    int32_t unit_rows;   // rows of a unit, on the average
     int32_t min_tiles;   // tiles of keys of a part, at least
-    float to_cap;        // from scores in units of log2 to the tanh's argument
+    float to_cap;        // from products to the tanh's argument
 };
 size_t prompt_workspace(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages);
 hipError_t launch_attend_prompt(int dt, const apc_kv& c, const PromptArgs& a, hipStream_t s);

@@ -3,11 +3,15 @@
 // kernel is in prompt_kernel.h.
 #include "prompt_kernel.h"
 
+#include <algorithm>
+#include <limits>
+
 namespace apc {
 namespace {
 
-// Joins the parts of units whose keys were cut, in the order of the parts: ROWS
-// rows a workgroup, the threads of a row over (some of the parts) x (elements).
+// Joins the parts of units whose keys were cut, in the order of the parts: a
+// workgroup takes ROWS rows of a unit at a time, and the threads of a row stand over
+// (some of the parts) x (elements).
 template <int DT, int DP, int ROWS>
 __global__ __launch_bounds__(256) void k_prompt_join(apc_kv c, PromptArgs a, PromptPlan p, int kt)
 {
@@ -19,73 +23,75 @@ __global__ __launch_bounds__(256) void k_prompt_join(apc_kv c, PromptArgs a, Pro
     const int head = blockIdx.x % c.heads, k = blockIdx.x / c.heads, group = a.q_heads / c.heads;
     const PromptUnit u = prompt_unit(a, group, p.rows, k);
     if (u.seq < 0) return;
-    const int all = u.n * group, r = blockIdx.y * ROWS + threadIdx.x / PER, row = u.tile * p.rows + r;
-    if (u.tile * p.rows + (int)blockIdx.y * ROWS >= all) return;
     const PromptSight sight(a, p.shift, group, u);
     const PromptKeys keys(p, sight, u, p.rows, kt);
     if (keys.parts == 1) return;
+    const int left = u.n * group - u.tile * p.rows, rows = left < p.rows ? left : p.rows;
     const int i = threadIdx.x / PER, part0 = threadIdx.x % PER / LANES, d = threadIdx.x % LANES * 4;
     const float* po = static_cast<const float*>(a.ws);
     const float* pm = po + prompt_slots(p, c.heads) * DP;
-    const bool mine = row < all;
-    const int64_t slot = prompt_slot(p, c.heads, k, head, 0) + (mine ? r : blockIdx.y * ROWS);
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    float top = LOWEST, sum = 0.f;
-    for (int q0 = part0; q0 < keys.parts; q0 += AT_ONCE * AHEAD) {
-        f32x4 x[AHEAD];
-        float m[AHEAD], l[AHEAD];
+    for (int r0 = blockIdx.y * ROWS; r0 < rows; r0 += gridDim.y * ROWS) {
+        const int r = r0 + i < rows ? r0 + i : r0;              // (a row past the end: the first one's, not stored)
+        const int64_t slot = prompt_slot(p, c.heads, k, head, 0) + r;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        float top = LOWEST, sum = 0.f;
+        for (int q0 = part0; q0 < keys.parts; q0 += AT_ONCE * AHEAD) {
+            f32x4 x[AHEAD];
+            float m[AHEAD], l[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const int q = q0 + j * AT_ONCE < keys.parts ? q0 + j * AT_ONCE : q0;
-            const int64_t at = slot + (int64_t)q * p.rows;
-            x[j] = *reinterpret_cast<const f32x4*>(po + at * DP + d);
-            m[j] = pm[at * 2];
-            l[j] = pm[at * 2 + 1];
+            for (int j = 0; j < AHEAD; ++j) {
+                const int q = q0 + j * AT_ONCE < keys.parts ? q0 + j * AT_ONCE : q0;
+                const int64_t at = slot + (int64_t)q * p.rows;
+                x[j] = *reinterpret_cast<const f32x4*>(po + at * DP + d);
+                m[j] = pm[at * 2];
+                l[j] = pm[at * 2 + 1];
+            }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                if (q0 + j * AT_ONCE >= keys.parts) break;
+                const float y = __builtin_fmaxf(top, m[j]);
+                const float was = __builtin_amdgcn_exp2f(top - y), is = __builtin_amdgcn_exp2f(m[j] - y);
+                v = v * was + x[j] * is;
+                sum = sum * was + l[j] * is;
+                top = y;
+            }
         }
+        if constexpr (AT_ONCE > 1) {
+            if (r0 != (int)blockIdx.y * ROWS) __syncthreads();
+            *reinterpret_cast<f32x4*>(&acc[i][part0][d]) = v;
+            if (d == 0) sums[i][part0] = sum, tops[i][part0] = top;
+            __syncthreads();
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            if (q0 + j * AT_ONCE >= keys.parts) break;
-            const float y = __builtin_fmaxf(top, m[j]);
-            const float was = __builtin_amdgcn_exp2f(top - y), is = __builtin_amdgcn_exp2f(m[j] - y);
-            v = v * was + x[j] * is;
-            sum = sum * was + l[j] * is;
-            top = y;
+            for (int j = 0; j < AT_ONCE; ++j) top = __builtin_fmaxf(top, tops[i][j]);
+            sum = 0.f;
+            v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const float f = __builtin_amdgcn_exp2f(tops[i][j] - top);
+                sum = __builtin_fmaf(f, sums[i][j], sum);
+                v += f * *reinterpret_cast<const f32x4*>(&acc[i][j][d]);
+            }
+        }
+        if (r0 + i < rows && part0 == 0) {
+            const float f = sum == 0.f ? 0.f : 1.0f / sum;
+            const float out[4] = {sum == 0.f ? 0.f : v.x * f, sum == 0.f ? 0.f : v.y * f, sum == 0.f ? 0.f : v.z * f,
+                                  sum == 0.f ? 0.f : v.w * f};
+            const int row = u.tile * p.rows + r, h = head * group + row % group;
+            const int64_t token = u.first + row / group;
+            if (d < c.d) store_values<DT, 4>(static_cast<T*>(a.out) + token * a.out_row + h * a.out_head + d, out);
+            if (a.lse && d == 0) a.lse[token * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
         }
     }
-    if constexpr (AT_ONCE > 1) {
-        *reinterpret_cast<f32x4*>(&acc[i][part0][d]) = v;
-        if (d == 0) sums[i][part0] = sum, tops[i][part0] = top;
-        __syncthreads();
-        if (part0 > 0) return;
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) top = __builtin_fmaxf(top, tops[i][j]);
-        sum = 0.f;
-        v = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            const float f = __builtin_amdgcn_exp2f(tops[i][j] - top);
-            sum = __builtin_fmaf(f, sums[i][j], sum);
-            v += f * *reinterpret_cast<const f32x4*>(&acc[i][j][d]);
-        }
-    }
-    if (!mine) return;
-    const float f = sum == 0.f ? 0.f : 1.0f / sum;
-    const float out[4] = {sum == 0.f ? 0.f : v.x * f, sum == 0.f ? 0.f : v.y * f, sum == 0.f ? 0.f : v.z * f,
-                          sum == 0.f ? 0.f : v.w * f};
-    const int64_t token = u.first + row / group;
-    const int h = head * group + row % group;
-    if (d < c.d) store_values<DT, 4>(static_cast<T*>(a.out) + token * a.out_row + h * a.out_head + d, out);
-    if (a.lse && d == 0) a.lse[token * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
 template <int DT, int DP> hipError_t join(const apc_kv& c, const PromptArgs& a, const PromptPlan& p, int kt, hipStream_t s)
 {
-    // few rows with many parts: a workgroup a row; else several rows
-    constexpr int MANY = DP > 128 ? 4 : 8;
-    const int rows = p.rows == 32 ? 1 : MANY;
-    const dim3 grid((unsigned)(p.tiles * c.heads), (unsigned)(p.rows / rows));
+    // many parts: a workgroup a row; else several rows
+    constexpr int SEVERAL = DP > 128 ? 4 : 8;
+    const int rows = p.splits > SEVERAL ? 1 : SEVERAL;
+    const dim3 grid((unsigned)(p.tiles * c.heads), (unsigned)((p.unit_rows + rows - 1) / rows));
     if (rows == 1) k_prompt_join<DT, DP, 1><<<grid, dim3(256), 0, s>>>(c, a, p, kt);
-    else k_prompt_join<DT, DP, MANY><<<grid, dim3(256), 0, s>>>(c, a, p, kt);
+    else k_prompt_join<DT, DP, SEVERAL><<<grid, dim3(256), 0, s>>>(c, a, p, kt);
     return hipGetLastError();
 }
 
@@ -93,27 +99,43 @@ int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 int tile_keys(int rows, int dp) { return rows == 32 || dp > 128 ? 32 : 64; }
 
 // Row tiles of 32, whose four waves share the keys out, where sequences have no
-// more rows than that on the average; else of 128, a wave 32 of them.
-constexpr int FEW_ROWS = 32;
-// Workgroups that keys are cut for where units are fewer, and keys of a part, at least
-int64_t wanted(int rows) { return rows == 32 ? 2048 : 512; }
-constexpr int MIN_KEYS = 512;
+// more rows than that on the average, or where tiles of 128, a wave 32 of them,
+// would be fewer than the CUs: a call of little work is the latency of its longest
+// wave's tiles (7 sequences of 1 to 333 tokens over e4m3, 5 x 2 heads of 80: 19 us,
+// 47 in 76 tiles of 128; 256 tokens, 4 x 8 heads of 128: 10.5 and 14; 512 tiles of 128 of
+// 1,024 tokens behind 64,512: 1,400 us, 2,540 in tiles of 32).
+constexpr int FEW_ROWS = 32, CUS = 256;
+// Keys are cut where units are fewer than the workgroups that the chip holds at
+// once (two a CU), into parts whose time is more than the join's.  Row tiles of 32
+// are cut further while parts stay long, so that ragged lengths leave less at the
+// end (64 single tokens over 16,384 to 32,768 tokens: 625 us, 670 in parts twice as long;
+// one over 131,072: 68, 92 in parts of 512 tokens).
+constexpr int FULL = 2 * CUS, MANY = 8 * CUS, LONG_KEYS = 4096;
+constexpr int min_keys(int rows) { return rows == 32 ? 512 : 1024; }
 
 int64_t row_tiles(int64_t t, int64_t b, int group, int rows) { return t * group / rows + (b < t ? b : t); }
-int64_t most_parts(int64_t max_pages, int page) { return max_pages * page / MIN_KEYS; }
+int64_t least_tiles(int64_t t, int64_t b, int group, int rows) { return std::max(std::min(b, t), (t * group + rows - 1) / rows); }
 
-PromptPlan plan(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages)
+PromptPlan plan(const apc_kv& c, const PromptArgs& a)
 {
     PromptPlan p{};
-    const int group = q_heads / c.heads;
+    const int group = a.q_heads / c.heads;
+    const int64_t t = a.t, b = a.b;
     while ((1 << p.shift) < c.page) ++p.shift;
     p.dp = padded(c.d);
+    const bool few = t * group <= FEW_ROWS * std::min(b, t) || least_tiles(t, b, group, 128) * c.heads < CUS;
     // (a launch has fewer than 2^32 threads)
-    p.rows = t * group <= FEW_ROWS * (b < t ? (int64_t)b : t) && row_tiles(t, b, group, 32) * c.heads < 1 << 23 ? 32 : 128;
+    p.rows = few && row_tiles(t, b, group, 32) * c.heads < 1 << 23 ? 32 : 128;
     p.tiles = (int32_t)row_tiles(t, b, group, p.rows);
-    const int64_t units = (int64_t)p.tiles * c.heads, most = most_parts(max_pages, c.page), want = wanted(p.rows) / units;
-    p.splits = (int32_t)(want < 1 || most < 1 ? 1 : want < most ? want : most);
-    p.min_tiles = MIN_KEYS / tile_keys(p.rows, p.dp);
+    const int64_t tiles = least_tiles(t, b, group, p.rows), units = tiles * c.heads;
+    // keys of a unit, at most
+    int64_t keys = (int64_t)a.max_pages * c.page;
+    if (a.window > 0) keys = std::min(keys, (a.prefix ? 2 : 1) * (int64_t)a.window + p.rows / group + 1);
+    int64_t splits = FULL / units;
+    if (p.rows == 32) splits = std::max(splits, std::min(MANY / units, keys / LONG_KEYS));
+    p.splits = (int32_t)std::max<int64_t>(1, std::min(splits, keys / min_keys(p.rows)));
+    p.unit_rows = (int32_t)std::min<int64_t>(p.rows, (t * group + tiles - 1) / tiles);
+    p.min_tiles = min_keys(p.rows) / tile_keys(p.rows, p.dp);
     return p;
 }
 
@@ -121,16 +143,16 @@ PromptPlan plan(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t 
 
 size_t prompt_workspace(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages)
 {
-    // what any call of up to so many tokens, sequences and pages can ask
-    const int64_t most = most_parts(max_pages, c.page);
-    if (t == 0 || b == 0 || most < 2) return 0;
+    // what any call of up to so many tokens, sequences and pages can ask: a plan's tiles
+    // are fewer than twice the least there can be, for which its parts are
+    if (t == 0 || b == 0) return 0;
     const int group = q_heads / c.heads;
     int64_t slots = 0;
     for (int rows : {32, 128}) {
-        if (rows == 128 && t * group <= FEW_ROWS) continue;
-        const int64_t units = row_tiles(t, b, group, rows) * c.heads;
-        const int64_t parts = units < wanted(rows) / most ? units * most : wanted(rows);
-        slots = parts * rows > slots ? parts * rows : slots;
+        if (rows > 32 && t * group <= FEW_ROWS) continue;
+        const int64_t most = (int64_t)max_pages * c.page / min_keys(rows), full = 2 * (rows == 32 ? MANY : FULL);
+        if (most < 2) continue;
+        slots = std::max(slots, std::min(row_tiles(t, b, group, rows) * c.heads * most, full) * rows);
     }
     return (size_t)slots * (padded(c.d) + 2) * sizeof(float);
 }
@@ -139,9 +161,11 @@ hipError_t launch_attend_prompt(int dt, const apc_kv& c, const PromptArgs& args,
 {
     if (args.b <= 0 || args.t <= 0) return hipSuccess;
     PromptArgs a = args;
-    PromptPlan p = plan(c, a.t, a.b, a.q_heads, a.max_pages);
+    PromptPlan p = plan(c, a);
     if (c.n_pages == 0) a.max_pages = 0;                        // no page to read from
-    if (a.cap > 0.f) p.to_cap = LN2 / a.cap;
+    // (a cap so far away bends nothing; so near, its inverse ends the range)
+    if (a.cap > 0x1p100f) a.cap = 0.f;
+    if (a.cap > 0.f) p.to_cap = std::min(std::fabs(a.scale) / a.cap, std::numeric_limits<float>::max());
     const hipError_t e = c.dt == APC_E4M3 ? launch_prompt_e4m3(dt, c, a, p, s)
                          : c.dt == APC_F16 ? launch_prompt_f16(c, a, p, s) : launch_prompt_bf16(c, a, p, s);
     if (e != hipSuccess || p.splits == 1) return e;

@@ -20,6 +20,15 @@
 // Two shapes: SHARED, where R waves have 32 rows each and the same keys (tiles in
 // two LDS buffers, the next on its way in registers); else KW waves have the same
 // 32 rows and every KW-th tile each, in an LDS buffer of their own.
+//
+// Bound, for long SHARED units, by the matrix unit and what it waits for: two
+// prompts of 8,192 tokens, 4 x 8 heads of 128, bf16, take 1,170 us, 0.94 PFLOP/s, its unit
+// busy 45% of the time at 1.9 GHz (a large bf16 product reaches 1.58 in a trace, at
+// 93% and 1.72 GHz); loads cost 150 us of it, the copies to LDS 90.  Tried and not
+// kept: 64 rows a wave (half of the LDS reads, but one wave a SIMD: 1,350 us), 8
+// waves to a tile (1,150; short calls 5 to 10% more), with loads two tiles ahead
+// (no less).  Single tokens are bound by memory: 64 of 16,384 to 32,768, e4m3, 625 us,
+// 5.3 TB/s (streaming reads reach 6.2).
 #pragma once
 
 #include "attend_common.h"
@@ -192,7 +201,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     constexpr int NT = SHARED ? 64 * R : 64;                    // threads that load a tile
     constexpr int CH = DP * ES / 16, RW = 64 / CH;              // 16-byte pieces of a row, rows of a wave's load
     constexpr int ITS = KT * CH / NT, STEP = NT / CH;           // loads of a thread, rows between them
-    constexpr int KS = DP + 8, VS = DP + 16;                    // elements between rows in LDS
+    constexpr int KS = DP + 8, VS = DP + 32;                    // elements between rows in LDS: reads meet every bank once
     constexpr int BUF = KT * (KS + VS) + (E8 ? 4 * KT : 0);     // of a buffer (16 bits each)
     constexpr int BUFS = SHARED ? 2 : KW;
     constexpr int JOIN = SHARED ? 0 : KW * (32 * (DP + 4) + 64) * 2;
@@ -220,6 +229,9 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     const int row = row0 + col < all ? row0 + col : all - 1;
     const int token = row / group, qh = head * group + row % group;
     const int at = sight.past + token, lo = sight.first(at), hi = sight.end(at);
+    float slope = a.slopes ? a.slopes[qh] : 0.f;
+    // (finite where the slope is: no distance times it is 0)
+    slope = __builtin_fabsf(slope) > 2.3e38f && __builtin_fabsf(slope) < INFINITY ? __builtin_copysignf(3.4e38f, slope) : slope * LOG2E;
 
     const int row_bytes = c.d * ES, in_page = c.page - 1;
     u32x4 q[DP / 16];
@@ -234,7 +246,6 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         }
     }
     const float sc = __builtin_fabsf(a.scale) * LOG2E;
-    const float slope = a.slopes ? a.slopes[qh] * LOG2E : 0.f;
 
     // keys and values on their way: 16-byte pieces of rows, zeros where there is no row
     const int32_t* table = a.pages + u.seq * a.ld_pages;
@@ -255,13 +266,21 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     struct Tile { u32x4 k[ITS], v[ITS]; float scale; };
     // a lane's place among the sixteen rows that its wave's load is in; past a row's end it reads the row's first piece
     const uint32_t place = (uint32_t)((row_of(0) % 16 + r_lane) * row_bytes + (in_row ? ch * 16 : 0));
+    const uint64_t page_bytes = ((uint64_t)c.heads << p.shift) * row_bytes, head_bytes = ((uint64_t)head << p.shift) * row_bytes;
     auto load = [&](Tile& to, int j0, int32_t pages) INLINE {
+        // a lane has the first of its key's sixteen rows, which those that load it take from there
+        const uint64_t rows = (uint32_t)pages * page_bytes + head_bytes + (uint32_t)((j0 + lane % KT / 16 * 16) & in_page) * row_bytes;
         auto one = [&](int it) INLINE {
-            const int j = j0 + row_of(it) / 16 * 16;
-            const int64_t base = first_row(page_of(pages, row_of(it)), j) * row_bytes;
+            const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)rows, row_of(it) / 16 * 16);
+            const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(rows >> 32), row_of(it) / 16 * 16);
+            const uint64_t base = (uint64_t)hi << 32 | lo;
+            using Bytes = const __attribute__((address_space(1))) uint8_t;
+            using Piece = const __attribute__((address_space(1))) u32x4;
+            Bytes *k = (Bytes*)c.k + base, *v = (Bytes*)c.v + base;
+            asm("" : "+s"(k), "+s"(v));                         // (the same for all lanes: no 64-bit sums in each)
             const uint32_t off = place + (uint32_t)(it * STEP % 16 * row_bytes);
-            to.k[it] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.k) + base + off);
-            to.v[it] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(c.v) + base + off);
+            to.k[it] = *(Piece*)(k + off);
+            to.v[it] = *(Piece*)(v + off);
         };
         if (__builtin_expect(all_there(pages, j0 + lane % KT / 16 * 16), 1)) {
 #pragma unroll
@@ -340,27 +359,38 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         const float* scales = reinterpret_cast<const float*>(from + KT * (KS + VS));
         if (j0 + KT <= lo_a || j0 >= hi_z) return;              // nothing that these rows see
         float s[KT / 32][16];
-        // operands from LDS, AHEAD of them on their way (left to itself the compiler waits for each before its product)
-        constexpr int NK = KT / 32 * (DP / 16), NV = KT / 16 * (DP / 32), AHEAD = 4;
+        // operands from LDS, so many of them on their way (left to itself the compiler waits for each before its
+        // product): what registers hold
+        constexpr int NK = KT / 32 * (DP / 16), NV = KT / 16 * (DP / 32);
+        constexpr int AHEAD_K = SHARED ? 8 : E8 ? 4 : 3, AHEAD = SHARED || E8 ? 4 : 2;
+        int eight = 8 * half;
+        if constexpr (CAREFUL) {                                // (else held in a register through the other loop for this one)
+            eight = threadIdx.x;
+            asm("" : "+v"(eight));
+            eight = eight >> 2 & 8;
+        }
         auto key_at = [&](int i) INLINE {                       // i: elements 16 (i / (KT / 32)) on of keys 32 (i % (KT / 32)) on
-            return *reinterpret_cast<const u32x4*>(kk + (i % (KT / 32) * 32 + col) * KS + i / (KT / 32) * 16 + 8 * half);
+            return *reinterpret_cast<const u32x4*>(kk + (i % (KT / 32) * 32 + col) * KS + i / (KT / 32) * 16 + eight);
         };
+        // (of two waves, the one with products to issue goes first: as equals both would wait for the same unit)
+        __builtin_amdgcn_s_setprio(1);
         {
-            u32x4 key[AHEAD];
+            u32x4 key[AHEAD_K];
             f32x16 sum[KT / 32];
 #pragma unroll
             for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum[b][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) key[i] = key_at(i);
-            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+            for (int i = 0; i < AHEAD_K; ++i) key[i] = key_at(i);
+            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD_K, 0);
 #pragma unroll
             for (int i = 0; i < NK; ++i) {
-                sum[i % (KT / 32)] = mfma32<QBF>(key[i % AHEAD], q[i / (KT / 32)], sum[i % (KT / 32)]);
+                constexpr int B = KT / 32;
+                sum[i % B] = mfma32<QBF>(key[i % AHEAD_K], q[i / B], sum[i % B]);
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                if (i + AHEAD < NK) {
-                    key[i % AHEAD] = key_at(i + AHEAD);
+                if (i + AHEAD_K < NK) {
+                    key[i % AHEAD_K] = key_at(i + AHEAD_K);
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
             }
@@ -369,78 +399,78 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[b][i] = sum[b][i];
         }
-        // scores in units of log2: s times f
+        __builtin_amdgcn_s_setprio(0);
         const bool whole = j0 >= lo_z && j0 + KT <= hi_a && all_there(pages, j0 + lane % KT);
-        float f = sc;
-        if (E8 || a.cap > 0.f || a.slopes || !whole) {
-            f = 1.f;
+        if constexpr (E8) {
 #pragma unroll
             for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
-                    f32x4 y = {sc, sc, sc, sc};
-                    if constexpr (E8) y *= *reinterpret_cast<const f32x4*>(scales + b * 32 + 2 * i + 4 * half);
+                    const f32x4 y = *reinterpret_cast<const f32x4*>(scales + b * 32 + 2 * i + 4 * half);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[b][i + e] *= y[e];
                 }
-            if (a.cap > 0.f) {
-                const float by = p.to_cap, cap = a.cap * LOG2E; // s by = x, tanh(x) cap
-                float top = 0.f;
+        }
+        float f = sc;                                           // s times f: scores in units of log2
+        if (a.cap > 0.f) {
+            float top = 0.f;
+#pragma unroll
+            for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, __builtin_fabsf(s[b][i]));
+            // where none of the wave's is far, without the exponentials (and more exactly)
+            if (!__any(!(top * p.to_cap <= NEAR))) {
 #pragma unroll
                 for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        s[b][i] *= by;
-                        top = __builtin_fmaxf(top, __builtin_fabsf(s[b][i]));
+                        const float x = s[b][i] * p.to_cap;
+                        s[b][i] = x * tanh_over_x(x * x);
                     }
-                // where none of the wave's is far, without the exponentials (and more exactly)
-                if (!__any(!(top <= NEAR))) {
+            } else {
 #pragma unroll
-                    for (int b = 0; b < KT / 32; ++b)
+                for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[b][i] *= cap * tanh_over_x(s[b][i] * s[b][i]);
-                } else {
+                    for (int i = 0; i < 16; ++i) {
+                        // (told apart from the other branch's, or the compiler computes all of the near
+                        // ones before the branch, and runs out of registers)
+                        float x = s[b][i];
+                        asm volatile("" : "+v"(x));
+                        x *= p.to_cap;
+                        const float z = __builtin_fabsf(x);
+                        const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * LOG2E * z));
+                        const float near = x * tanh_over_x(x * x), y = __builtin_copysignf(far, x);
+                        s[b][i] = z <= NEAR ? near : y;
+                    }
+            }
+            f = a.cap * LOG2E;
+        }
+        if (a.slopes) {
+            float away = (float)(at - j0 - 4 * half);           // of the lane's first key; exact where the product matters
+            asm volatile("" : "+v"(away));
 #pragma unroll
-                    for (int b = 0; b < KT / 32; ++b)
+            for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            // (told apart from the other branch's, or the compiler computes all of the near
-                            // ones before the branch, and runs out of registers)
-                            float x = s[b][i];
-                            asm volatile("" : "+v"(x));
-                            const float z = __builtin_fabsf(x);
-                            const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * LOG2E * z));
-                            const float near = x * tanh_over_x(x * x), y = __builtin_copysignf(far, x);
-                            s[b][i] = cap * (z <= NEAR ? near : y);
-                        }
+                for (int i = 0; i < 16; ++i) {
+                    const float far = __builtin_fabsf(away - (float)(b * 32 + i / 4 * 8 + i % 4));
+                    s[b][i] = __builtin_fmaf(-slope, far, s[b][i] * f);
                 }
-            }
-            if (a.slopes) {
-                float away = (float)(at - j0 - 4 * half);       // of the lane's first key; exact where the product matters
-                asm volatile("" : "+v"(away));
+            f = 1.f;
+        }
+        if (!whole) {
+            // of the lane's keys, `width` from `from` on, without the sixteens whose page is not there
+            int from = lo - j0 - 4 * half;
+            const int width = hi > lo ? hi - lo : 0;
+            asm volatile("" : "+v"(from));                      // (or the loop would keep every key's distance from `lo`)
+            const float by = f;
+            f = 1.f;                                            // (-inf times a scale of 0 is none)
 #pragma unroll
-                for (int b = 0; b < KT / 32; ++b)
+            for (int g = 0; g < KT / 16; ++g) {
+                const uint32_t seen = there(page_of(pages, g * 16), j0 + g * 16) ? (uint32_t)width : 0;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        s[b][i] = __builtin_fmaf(-slope, __builtin_fabsf(away - (float)(b * 32 + i / 4 * 8 + i % 4)), s[b][i]);
-            }
-            if (!whole) {
-                // of the lane's keys, those from `from` to `to` on; sixteens whose page is not there
-                int from = lo - j0 - 4 * half;
-                const int width = hi > lo ? hi - lo : 0;
-                asm volatile("" : "+v"(from));                  // (or the loop would keep every key's distance from `lo`)
-#pragma unroll
-                for (int b = 0; b < KT / 32; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint32_t at = (uint32_t)(b * 32 + i / 4 * 8 + i % 4 - from);
-                        s[b][i] = at < (uint32_t)width ? s[b][i] : -INFINITY;
-                    }
-#pragma unroll
-                for (int g = 0; g < KT / 16; ++g) {
-                    if (there(page_of(pages, g * 16), j0 + g * 16)) continue;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) s[g / 2][g % 2 * 8 + i] = -INFINITY;
+                for (int i = g % 2 * 8; i < g % 2 * 8 + 8; ++i) {
+                    const uint32_t at = (uint32_t)(g / 2 * 32 + i / 4 * 8 + i % 4 - from);
+                    s[g / 2][i] = at < seen ? s[g / 2][i] * by : -INFINITY;
                 }
             }
         }
@@ -450,7 +480,9 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, s[b][i]);
-        top = top * f - OFF;
+        top = top * f;
+        asm("" : "+v"(top));                                    // (rounded here, as below)
+        top -= OFF;
         if (__any(top > m + (CAREFUL ? 0.f : SLACK))) {
             const float y = both_halves_max(__builtin_fmaxf(m, top)), by = __builtin_amdgcn_exp2f(m - y);
             m = y;
@@ -458,44 +490,45 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
 #pragma unroll
             for (int b = 0; b < DP / 32; ++b) o[b] *= by;
         }
-        // weights
-        float l1 = 0.f;
+        // Where a step of float32 at the maximum's size is a good part of 1: the difference of rounded scores, so that the
+        // largest is near 0, and no more than weights are meant to reach (the scores are no better known there).
+        float less = m;
+        if (__builtin_expect(__any((m > LOWEST) & (__builtin_fabsf(m) > 0x1p22f)), 0)) {
+            constexpr float TOP = OFF + (CAREFUL ? 0.f : SLACK);
 #pragma unroll
-        for (int b = 0; b < KT / 32; ++b)
+            for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], f, -m));
-                (i % 2 ? l1 : l) += w;
-                s[b][i] = CAREFUL && s[b][i] == -INFINITY ? -1.f : w;   // (careful: none, told from 0)
-            }
-        l += l1;
-        u32x4 hi8[KT / 16], lo8[TWO ? KT / 16 : 1], any8[CAREFUL ? KT / 16 : 1];
-#pragma unroll
-        for (int x = 0; x < KT / 16; ++x) {
-            f32x4 y[2] = {{1.f, 1.f, 1.f, 1.f}, {1.f, 1.f, 1.f, 1.f}};
-            if constexpr (E8) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) y[i] = *reinterpret_cast<const f32x4*>(scales + KT + x * 16 + 8 * i + 4 * half);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float w0 = s[x / 2][x % 2 * 8 + 2 * i], w1 = s[x / 2][x % 2 * 8 + 2 * i + 1];
-                if constexpr (CAREFUL) {
-                    any8[x][i] = pack<PBF>(w0 < 0.f ? 0.f : 1.f, w1 < 0.f ? 0.f : 1.f);
-                    w0 = w0 < 0.f ? 0.f : E8 ? w0 * y[i / 2][i % 2 * 2] : w0;
-                    w1 = w1 < 0.f ? 0.f : E8 ? w1 * y[i / 2][i % 2 * 2 + 1] : w1;
-                } else if constexpr (E8) {
-                    w0 *= y[i / 2][i % 2 * 2], w1 *= y[i / 2][i % 2 * 2 + 1];
+                for (int i = 0; i < 16; ++i) {
+                    float x = s[b][i] * f;
+                    asm("" : "+v"(x));
+                    x -= m;
+                    s[b][i] = x > TOP ? TOP : x;
                 }
-                hi8[x][i] = pack<PBF>(w0, w1);
-                if constexpr (TWO) {
-                    const f32x2 z = unpack<PBF>(hi8[x][i]);
-                    lo8[x][i] = pack<PBF>(w0 - z.x, w1 - z.y);
-                    if constexpr (CAREFUL) lo8[x][i] &= ~not_finite<PBF>(hi8[x][i]);
-                }
-            }
+            f = 1.f, less = 0.f;
         }
-        // values: columns of the keys whose weights the lane has
+        // weights, of 16 keys at a time, and their values: columns of the keys whose weights the lane has
+        u32x4 hi8[KT / 16], lo8[TWO ? KT / 16 : 1], any8[CAREFUL ? KT / 16 : 1];
+        float l1 = 0.f;
+        auto weigh = [&](int x, int i) INLINE {                 // keys 2 i and 2 i + 1 of the lane's eight
+            const float s0 = s[x / 2][x % 2 * 8 + 2 * i], s1 = s[x / 2][x % 2 * 8 + 2 * i + 1];
+            float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s0, f, -less)), w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s1, f, -less));
+            l += w0, (SHARED ? l1 : l) += w1;                     // (two sums wait less, where there is a register)
+            f32x2 y = {1.f, 1.f};
+            if constexpr (E8) y = *reinterpret_cast<const f32x2*>(scales + KT + x * 16 + i / 2 * 8 + i % 2 * 2 + 4 * half);
+            if constexpr (CAREFUL) {
+                const bool n0 = s0 == -INFINITY, n1 = s1 == -INFINITY;          // (none, told from a weight of 0)
+                any8[x][i] = pack<PBF>(n0 ? 0.f : 1.f, n1 ? 0.f : 1.f);
+                w0 = n0 ? 0.f : w0 * y.x, w1 = n1 ? 0.f : w1 * y.y;
+            } else {
+                w0 *= y.x, w1 *= y.y;
+            }
+            hi8[x][i] = pack<PBF>(w0, w1);
+            if constexpr (TWO) {
+                const f32x2 z = unpack<PBF>(hi8[x][i]);
+                lo8[x][i] = pack<PBF>(w0 - z.x, w1 - z.y);
+                if constexpr (CAREFUL) lo8[x][i] &= ~not_finite<PBF>(hi8[x][i]);
+            }
+        };
         const uint16_t* column = vv + (4 * half + (lane & 15) / 4) * VS + (lane >> 4 & 1) * 16 + lane % 4 * 4;
         auto values_at = [&](int i) INLINE {                    // i: elements 32 (i % (DP / 32)) on of keys 16 (i / (DP / 32)) on
             const uint16_t* from = column + i / (DP / 32) * 16 * VS + i % (DP / 32) * 32;
@@ -503,22 +536,38 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             return u32x4{y.x, y.y, z.x, z.y};
         };
         if constexpr (!CAREFUL) {
+            // the next sixteen's weights are computed beside this one's products
+            constexpr bool BESIDE = SHARED;
             u32x4 v[AHEAD];
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int x = 0; x < (BESIDE ? 1 : KT / 16); ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) weigh(x, i);
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) v[i] = values_at(i);
             __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int x = i / (DP / 32), b = i % (DP / 32);
+                constexpr int B = DP / 32;
+                const int x = i / B, b = i % B;
+                if constexpr (BESIDE) __builtin_amdgcn_sched_barrier(0);
                 o[b] = mfma32<PBF>(v[i % AHEAD], hi8[x], o[b]);
                 if constexpr (TWO) o[b] = mfma32<PBF>(v[i % AHEAD], lo8[x], o[b]);
-                __builtin_amdgcn_sched_group_barrier(0x008, TWO ? 2 : 1, 0);
+                if constexpr (!BESIDE) __builtin_amdgcn_sched_group_barrier(0x008, TWO ? 2 : 1, 0);
                 if (i + AHEAD < NV) {
                     v[i % AHEAD] = values_at(i + AHEAD);
-                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    if constexpr (!BESIDE) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                 }
+                if (BESIDE && x + 1 < KT / 16)
+#pragma unroll
+                    for (int j = 4 * b / B; j < 4 * (b + 1) / B; ++j) weigh(x + 1, j);
             }
         } else {
+#pragma unroll
+            for (int x = 0; x < KT / 16; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) weigh(x, i);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 // infinite and NaN values by kind, where a weight is for them; else 0 in their place
@@ -541,6 +590,8 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
                 if constexpr (TWO) o[b] = mfma32<PBF>(v, lo8[x], o[b]);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
+        l += l1;
     };
     auto not_finite_out = [&]() INLINE {
         float z = 0.f;
@@ -690,7 +741,9 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             return;
         }
         const float f = sum == 0.f ? 0.f : 1.0f / sum;
-        const int tok = mine / group, h = head * group + mine % group;
+        int by = group;
+        asm("" : "+s"(by));                                     // (else its inverse is held in a register through the loop)
+        const int tok = mine / by, h = head * group + mine % by;
         T* const to = static_cast<T*>(a.out) + (u.first + tok) * a.out_row + h * a.out_head + d0;
         constexpr int ST = OWN < 16 ? OWN : 16;                 // d is a multiple of 16
 #pragma unroll

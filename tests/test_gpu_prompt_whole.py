@@ -421,6 +421,61 @@ def test_prompt_light_weights(apc, orc, cache, dtype):
         check_prompt(orc, cache, dtype, *made, 1.0, *run_prompt(apc, *made, 1.0))
 
 
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("slope", [1e6, 1e30, 3e38])
+def test_prompt_steep_slopes(apc, orc, cache, dtype, slope):
+    """Slopes that leave each token itself alone: its value, and its own score, whose bias is 0 however far the tile's
+    first key (distances above 0 lower a score by 1e6 and more, where scores are below 1e3)."""
+    for sizes in (SIZES, FEW):
+        say(f"prompt slope {slope} {dtype} over {cache} n={len(sizes)}")
+        made = make_prompt(51, sizes, 1, 2, 64, 16, 13, cache, dtype)
+        slopes = torch.full((2,), slope, device="cuda")
+        out, lse = run_prompt(apc, *made, 0.125, slopes=slopes)
+        alone, one = run_prompt(apc, *made, 0.125, window=1)
+        at = torch.isfinite(one) & (one != 7)
+        # Both calls leave each row the value v of one token: (w (1 + a) v / w) (1 + b), where the weight w enters the product
+        # rounded to the type (|a| <= half a step: exp2 of a rounded difference need not be a power of two) and the sum
+        # unrounded, and the output is rounded (|b| <= half a step).  So each is within 2 ROUND (1 + ROUND) |v| of v, and
+        # the two are within 4 ROUND |v| of each other, 1 + 4 ROUND for |v| from a result and second orders, below 1.04.
+        assert torch.equal(torch.isfinite(lse), torch.isfinite(one))
+        d = (out.float() - alone.float()).abs()[at]
+        assert (d <= 4.16 * ROUND[dtype] * alone.float().abs()[at] + TINY[dtype]).all(), (d / alone.float().abs()[at]).max()
+        assert (lse - one)[at].abs().max() < 1e-4
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("size", [1e7, 1e9, 1e12, 1e30])
+def test_prompt_huge_scores(apc, cache, dtype, size):
+    """Scores whose float32 steps are many times 1: the result is a mean of the values with weights that are finite (any,
+    as no score is known to better than a step), and 0 where nothing is seen."""
+    for sizes in (SIZES, FEW):
+        say(f"prompt scores of {size} {dtype} over {cache} n={len(sizes)}")
+        pool, table, q, starts, lens = made = make_prompt(57, sizes, 1, 2, 64, 16, 13, cache, dtype)
+        out, lse = run_prompt(apc, *made, size)
+        _, one = run_prompt(apc, *made, 0.0)
+        v = pool[1].float() if pool[3] is None else pool[1].float() * pool[3][..., None]
+        assert torch.isfinite(out.float()).all() and torch.equal(torch.isfinite(lse), torch.isfinite(one))
+        # a mean lies within the values; its weights and itself are rounded
+        assert out.float().abs().max() <= v.abs().max() * (1 + 3 * ROUND[dtype])
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+def test_prompt_cap_ends(apc, orc, cache, dtype):
+    """Caps so small that every score is 0 but for less than float32 tells, and so large that none is bent."""
+    for sizes in (SIZES, FEW):
+        made = make_prompt(53, sizes, 2, 2, 64, 16, 13, cache, dtype)
+        for cap in (1e-30, 1e-44, 1e30, 2e30, 3.4e38):
+            say(f"prompt cap {cap} {dtype} over {cache} n={len(sizes)}")
+            if cap < 1:
+                check_prompt(orc, cache, dtype, *made, 0.0, *run_prompt(apc, *made, 0.125, cap=cap))
+            else:
+                # (tanh is linear there: float32 carries x / cap as exactly as x)
+                got, want = run_prompt(apc, *made, 0.125, cap=cap), run_prompt(apc, *made, 0.125)
+                some = torch.isfinite(want[1])
+                assert (got[1] - want[1])[some].abs().max() < 1e-4
+                assert ((got[0].float() - want[0].float()).abs() <= 4 * ROUND[dtype] * want[0].float().abs() + 4 * ROUND[dtype] * 3.0).all()
+
+
 def test_prompt_views(apc, orc):
     """Queries inside a fused product's rows, head-major outputs, page tables inside wider ones, no lse."""
     pool, table, q, starts, lens = make_prompt(41, SIZES, 2, 4, 80, 16, 13, "bf16", "bf16", pad=2)
