@@ -821,7 +821,7 @@ apc_status apc_rotate(const apc_rotary* r, apc_dtype dt, int64_t t, int32_t head
     if ((heads > 1 && out_head < d) || (t > 1 && out_tok < d) || (heads > 1 && t > 1 && out_head == out_tok))
         return fail(APC_E_ARG, "apc_rotate: rows of out overlap");
     const apc::RotateArgs a{x, out, positions, r->freq, t, x_tok, x_head, out_tok, out_head, heads, d, r->rot, r->mag,
-                            r->interleaved != 0, false};
+                            r->interleaved != 0, false, false};
     hipError_t err = apc::launch_rotate(dt, a, static_cast<hipStream_t>(stream));
     if (err != hipSuccess) return hip_fail(err, "apc_rotate launch");
     return ok();

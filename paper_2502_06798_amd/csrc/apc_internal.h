@@ -93,7 +93,7 @@ struct RotateArgs {
     int64_t t, x_tok, x_head, out_tok, out_head;    // strides in elements
     int32_t heads, d, rot;
     float mag;
-    bool interleaved, past;                         // past: outputs go past the caches
+    bool interleaved, past, in_place;               // past: outputs go past the caches; both are launch_rotate's
 };
 hipError_t launch_rotate(int dt, const RotateArgs& a, hipStream_t s);
 

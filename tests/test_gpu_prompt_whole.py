@@ -566,6 +566,59 @@ def test_prompt_streams_and_graph(apc):
             assert torch.equal(w["out"], o) and torch.equal(w["lse"], l)
 
 
+@pytest.mark.parametrize("cache,dtype", KINDS)
+def test_prompt_layer_whole_in_pieces_and_by_tokens(apc, orc, cache, dtype):
+    """A layer's calls as a text model makes them: queries and keys of a fused product's output turned in place, keys and
+    values written, attention; whole prompts, the same in two pieces, and the last tokens alone by apc_attend."""
+    heads, group, d, page, hq = 2, 3, 64, 16, 6
+    lens = [40, 1, 77, 17]
+    t, b, per = sum(lens), len(lens), 5
+    g = gen(61)
+    qkv = torch.randn((t, hq + 2 * heads, d), device="cuda", generator=g).to(TORCH[dtype])
+    at = torch.cat([torch.arange(n) for n in lens]).to(torch.int32).cuda()
+    seq = torch.repeat_interleave(torch.arange(b), torch.tensor(lens)).cuda()
+    table = torch.randperm(b * per, device="cuda", generator=g).to(torch.int32).view(b, per)
+    slots = table[seq, (at // page).long()] * page + at % page
+    freq = torch.from_numpy(apc.apc_rotary_freqs(d)).cuda()
+    rotary = apc.Rotary(freq)
+    was = f64(qkv[:, :hq + heads])
+    apc.apc_rotate(rotary, qkv[:, :hq + heads], at, qkv[:, :hq + heads])
+    torch.cuda.synchronize()
+    check_rotate(orc, was, at.cpu().numpy(), freq.cpu().numpy(), False, 1.0, f64(qkv[:, :hq + heads]), dtype)
+    q, k, v = qkv.split([hq, heads, heads], dim=1)
+    pool = make_pool(b * per, heads, page, d, cache)
+    c = apc.KvCache(*pool)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    bounds = np.concatenate([[0], np.cumsum(lens)])
+    ws = apc.attend_prompt_workspace_tensor(c, t, b, hq, per)
+
+    def attend(rows, new, length):
+        out, lse = torch.full((len(rows), hq, d), 7.0, device="cuda").to(q.dtype), torch.full((len(rows), hq), 7.0, device="cuda")
+        qq, starts = q[rows], i32(np.concatenate([[0], np.cumsum(new)]).tolist())
+        apc.apc_attend_prompt(c, qq, starts, table, i32(length), d ** -0.5, out, ws, lse)
+        torch.cuda.synchronize()
+        check_prompt(orc, cache, dtype, pool, table, qq, starts, i32(length), d ** -0.5, out, lse)
+        return out
+
+    apc.apc_kv_write(c, k, v, slots)
+    whole = attend(torch.arange(t, device="cuda"), lens, lens)
+    last = torch.from_numpy(bounds[1:] - 1).cuda()
+    alone, lse = torch.empty((b, hq, d), device="cuda").to(q.dtype), torch.empty((b, hq), device="cuda")
+    apc.apc_attend(c, q[last], table, i32(lens), d ** -0.5, alone, apc.attend_workspace_tensor(c, b, hq, per), lse)
+    torch.cuda.synchronize()
+    # (each within the weights' and the output's rounding of the mean: 2 ROUND of values below 6, and so twice that apart)
+    assert (alone.float() - whole[last].float()).abs().max() <= 4 * ROUND[dtype] * 6
+    for p in pool:
+        if p is not None:
+            p.view(torch.uint8).zero_()
+    first = [n // 3 for n in lens]
+    for lo, hi in (([0] * b, first), (first, lens)):
+        rows = torch.cat([torch.arange(s + a, s + e) for s, a, e in zip(bounds, lo, hi)]).cuda()
+        apc.apc_kv_write(c, k[rows], v[rows], slots[rows])
+        out = attend(rows, [e - a for a, e in zip(lo, hi)], hi)
+        assert (out.float() - whole[rows].float()).abs().max() <= 4 * ROUND[dtype] * 6
+
+
 def test_prompt_results_do_not_depend_on_the_run(apc):
     """The same call again: bit for bit, also where keys are cut into parts."""
     made = make_prompt(47, [(1, 9000), (150, 8000)], 2, 4, 128, 64, 141, "e4m3", "bf16")
