@@ -624,8 +624,8 @@ apc_status apc_attend_prompt_workspace(const apc_kv* c /* host */, int64_t t, in
  * range, takes longer).
  * Scores, the running maximum and sum and the output's sums are float32.  The
  * weights of the values enter the matrix product rounded to the type of q (an
- * error of half a step of each weight), or, for f16 over an e4m3 cache and where
- * sequences have few new tokens, in two parts (2^-16 of a weight); over f16
+ * error of half a step of each weight), or, for f16 over an e4m3 cache, where
+ * sequences have few new tokens and in small calls, in two parts (2^-16 of a weight); over f16
  * caches a weight below 2^-25 of its row's heaviest loses bits, and below 2^-36
  * counts as 0.
  * dt          type of q and out: the cache's, or APC_F16 / APC_BF16 where the
