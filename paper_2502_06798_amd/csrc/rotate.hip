@@ -41,14 +41,15 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a, int chunks, int co
     const int64_t per_token = (int64_t)per_head * groups, total = a.t * per_token;
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += (int64_t)gridDim.x * 256) {
         const int64_t token = quotient(id, per_token);
-        const int in = (int)(id - token * per_token), chunk = in % per_head, head0 = in / per_head;
+        const int64_t in = id - token * per_token, head0 = quotient(in, per_head);     // (heads may be 2^31 - 1)
+        const int chunk = (int)(in - head0 * per_head);
         const int position = a.positions[token];
         if (position < 0) continue;
         const T* x = static_cast<const T*>(a.x) + token * a.x_tok;
         T* out = static_cast<T*>(a.out) + token * a.out_tok;
         if (chunk >= chunks) {
             const int d0 = a.rot + (chunk - chunks) * V, n = a.d - d0 < V ? a.d - d0 : V;
-            for (int h = head0; h < a.heads; h += groups) {
+            for (int64_t h = head0; h < a.heads; h += groups) {
                 const T* from = x + h * a.x_head + d0;
                 T* to = out + h * a.out_head + d0;
                 if (n == V) {
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a, int chunks, int co
             s[i] *= a.mag, c[i] *= a.mag;
         }
         const int d0 = PAIRS ? 2 * p0 : p0, d1 = p0 + half;
-        for (int h = head0; h < a.heads; h += groups) {
+        for (int64_t h = head0; h < a.heads; h += groups) {
             const T* from = x + h * a.x_head;
             T* to = out + h * a.out_head;
             if constexpr (PAIRS) {
@@ -117,7 +118,7 @@ template <int DT, int V> hipError_t launch(const RotateArgs& a, hipStream_t s)
     // one head a thread until the chip is full, then up to four, which share the sines
     const int64_t threads = a.t * a.heads * (chunks + copies);
     const int heads_each = threads >= 4 << 19 ? 4 : threads >= 2 << 19 ? 2 : 1;
-    const int groups = (a.heads + heads_each - 1) / heads_each;
+    const int groups = (int)(((int64_t)a.heads + heads_each - 1) / heads_each);
     const int64_t blocks = (a.t * groups * (chunks + copies) + 255) / 256;
     const dim3 grid((unsigned)(blocks < MAX_GRID ? blocks : MAX_GRID));
     if (!a.interleaved) k_rotate<DT, false, V><<<grid, dim3(256), 0, s>>>(a, chunks, copies, groups);

@@ -137,6 +137,23 @@ def test_rotate_large(apc):
         assert torch.equal(part.view(torch.int16), out[i0:i0 + 500].view(torch.int16))
 
 
+def test_rotate_as_many_heads_as_a_call_takes(apc, orc):
+    """One token of 2^31 - 1 heads: the last ones are turned, what lies between them is."""
+    heads, d = 2 ** 31 - 1, 2
+    x = torch.zeros((1, heads, d), device="cuda", dtype=torch.float16)
+    some = torch.cat([torch.arange(7), torch.arange(2 ** 30 - 3, 2 ** 30 + 3), torch.arange(heads - 7, heads)]).cuda()
+    was = torch.randn((1, len(some), d), device="cuda", generator=gen(8)).half()
+    x[:, some] = was
+    at = torch.tensor([12345], dtype=torch.int32, device="cuda")
+    freq = torch.from_numpy(apc.apc_rotary_freqs(2)).cuda()
+    say("rotate 2^31 - 1 heads in place")
+    apc.apc_rotate(apc.Rotary(freq), x, at, x)
+    torch.cuda.synchronize()
+    check_rotate(orc, f64(was), [12345], freq.cpu().numpy(), False, 1.0, f64(x[:, some]), "f16")
+    x[:, some] = 0
+    assert not any(x[0, i:i + 2 ** 28].any() for i in range(0, heads, 2 ** 28))
+
+
 # ---- attention -----------------------------------------------------------------
 
 def make_prompt(seed, sizes, heads, group, d, page, max_pages, cache, dtype, spread=1.0, pad=0):
