@@ -118,6 +118,7 @@ struct PromptPlan {
     int32_t min_tiles;   // tiles of keys of a part, at least
     float to_cap;        // from products to the tanh's argument
 };
+PromptPlan plan_prompt(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages, int32_t window, bool prefix);
 size_t prompt_workspace(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages);
 hipError_t launch_attend_prompt(int dt, const apc_kv& c, const PromptArgs& a, hipStream_t s);
 hipError_t launch_prompt_f16(const apc_kv& c, const PromptArgs& a, const PromptPlan& p, hipStream_t s);

@@ -116,21 +116,22 @@ constexpr int min_keys(int rows) { return rows == 32 ? 512 : 1024; }
 int64_t row_tiles(int64_t t, int64_t b, int group, int rows) { return t * group / rows + (b < t ? b : t); }
 int64_t least_tiles(int64_t t, int64_t b, int group, int rows) { return std::max(std::min(b, t), (t * group + rows - 1) / rows); }
 
-PromptPlan plan(const apc_kv& c, const PromptArgs& a)
+}  // namespace
+
+PromptPlan plan_prompt(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages, int32_t window, bool prefix)
 {
     PromptPlan p{};
-    const int group = a.q_heads / c.heads;
-    const int64_t t = a.t, b = a.b;
+    const int group = q_heads / c.heads;
     while ((1 << p.shift) < c.page) ++p.shift;
     p.dp = padded(c.d);
-    const bool few = t * group <= FEW_ROWS * std::min(b, t) || least_tiles(t, b, group, 128) * c.heads < CUS;
+    const bool few = t * group <= FEW_ROWS * std::min<int64_t>(b, t) || least_tiles(t, b, group, 128) * c.heads < CUS;
     // (a launch has fewer than 2^32 threads)
     p.rows = few && row_tiles(t, b, group, 32) * c.heads < 1 << 23 ? 32 : 128;
     p.tiles = (int32_t)row_tiles(t, b, group, p.rows);
     const int64_t tiles = least_tiles(t, b, group, p.rows), units = tiles * c.heads;
     // keys of a unit, at most
-    int64_t keys = (int64_t)a.max_pages * c.page;
-    if (a.window > 0) keys = std::min(keys, (a.prefix ? 2 : 1) * (int64_t)a.window + p.rows / group + 1);
+    int64_t keys = (int64_t)max_pages * c.page;
+    if (window > 0) keys = std::min(keys, (prefix ? 2 : 1) * (int64_t)window + p.rows / group + 1);
     int64_t splits = FULL / units;
     if (p.rows == 32) splits = std::max(splits, std::min(MANY / units, keys / LONG_KEYS));
     p.splits = (int32_t)std::max<int64_t>(1, std::min(splits, keys / min_keys(p.rows)));
@@ -138,8 +139,6 @@ PromptPlan plan(const apc_kv& c, const PromptArgs& a)
     p.min_tiles = min_keys(p.rows) / tile_keys(p.rows, p.dp);
     return p;
 }
-
-}  // namespace
 
 size_t prompt_workspace(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages)
 {
@@ -161,7 +160,7 @@ hipError_t launch_attend_prompt(int dt, const apc_kv& c, const PromptArgs& args,
 {
     if (args.b <= 0 || args.t <= 0) return hipSuccess;
     PromptArgs a = args;
-    PromptPlan p = plan(c, a);
+    PromptPlan p = plan_prompt(c, a.t, a.b, a.q_heads, a.max_pages, a.window, a.prefix != nullptr);
     if (c.n_pages == 0) a.max_pages = 0;                        // no page to read from
     // (a cap so far away bends nothing; so near, its inverse ends the range)
     if (a.cap > 0x1p100f) a.cap = 0.f;
