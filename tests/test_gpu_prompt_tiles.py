@@ -1,7 +1,7 @@
-"""GPU parity of attention of several new tokens where its rows make tiles of 128
-(four waves that share their keys), whose calls have at least 256 tiles times
-key-value heads: the float64 oracle, or what the call said before a change that
-must not reach it.
+"""GPU parity of attention of several new tokens by the row tiles that a call
+takes: those of 128 (four waves that share their keys) where there are at least
+256 tiles times key-value heads, else those of 32; against the float64 oracle, or
+what the call said before a change that must not reach it.
 
 Tolerances as in test_gpu_prompt_whole.py, the weights' part by the plan that
 the call takes: half a step of the type where one part carries a weight, 2^-16
@@ -18,7 +18,8 @@ import torch
 from tests.gpu_check import say
 from tests.prompt_plan import plan_of
 from tests.test_gpu_prompt_ops import KINDS, ROUND, TINY, U, f64, gen, stored
-from tests.test_gpu_prompt_whole import RULES, make_prompt, run_prompt
+from tests.test_gpu_prompt_whole import FEW, RULES, make_prompt, run_prompt
+from tests.test_gpu_prompt_whole import SIZES as SMALL
 
 pytestmark = pytest.mark.gpu
 
@@ -140,6 +141,32 @@ def test_tiles_absent_pages_and_odd_tables(apc, orc, cache, dtype, d):
     for kw in (dict(), dict(prefix=pre), dict(window=30, prefix=pre)):
         say(f"tiles absent {dtype} over {cache} d={d} {list(kw)}")
         check(orc, cache, dtype, tall(made, cache, **kw), 0.2, run_prompt(apc, *made, 0.2, **kw), heads=[0, 9, 37], **kw)
+
+
+STARTS = {"cut": [-4, 37, 60, 60, 10 ** 6, 10 ** 6 + 5, 2 ** 31 - 1], "falling": [100, 140, 143, 20, 60, 90, -3],
+          "turned": [2 ** 31 - 1, 150, 230, 40, 150, 3, -2 ** 31]}
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("name", STARTS)
+@pytest.mark.parametrize("heads", [2, 128])
+def test_starts_are_cut_and_falling_ones_have_no_row(apc, orc, cache, dtype, name, heads):
+    """Starts outside the rows, falling ones among them (no row stands in two sequences): sequences' rows are right, and
+    the others stay as they were."""
+    say(f"starts {name} {dtype} over {cache} heads={heads}")
+    pool, table, q, _, lens = make_prompt(71, [(40, 200), (30, 150), (60, 208), (50, 60), (40, 90), (35, 40)], heads, 2, 64, 16, 13, cache, dtype)
+    starts = torch.tensor(STARTS[name], dtype=torch.int32, device="cuda")
+    made = pool, table, q, starts, lens
+    assert plan_of(made, cache).rows == (32 if heads == 2 else 128)
+    some = [0, 1] if heads == 2 else [0, 50, 127]
+    cut = starts.clamp(0, q.shape[0]).tolist()
+    rows = [r for a, b in zip(cut, cut[1:]) for r in range(a, b)]
+    assert len(set(rows)) == len(rows) and (name == "cut" or 0 < len(rows) < q.shape[0])
+    for kw in (dict(), dict(prefix=torch.tensor([5, 0, 300, 9, 2, 40], dtype=torch.int32, device="cuda"), window=50)):
+        got = run_prompt(apc, *made, 0.2, **kw)
+        check(orc, cache, dtype, made, 0.2, got, heads=some, **kw)
+        rest = [r for r in range(q.shape[0]) if r not in set(rows)]
+        assert (got[0][rest] == 7).all() and (got[1][rest] == 7).all()
 
 
 def spoil(pool, keep, fill):
