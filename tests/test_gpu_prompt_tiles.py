@@ -143,6 +143,17 @@ def test_tiles_absent_pages_and_odd_tables(apc, orc, cache, dtype, d):
         check(orc, cache, dtype, tall(made, cache, **kw), 0.2, run_prompt(apc, *made, 0.2, **kw), heads=[0, 9, 37], **kw)
 
 
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("heads,group,d,page", [(2, 4, 64, 16), (2, 5, 80, 16), (1, 8, 128, 64), (1, 7, 256, 16), (3, 1, 48, 32)])
+def test_small_calls_carry_weights_in_two_parts(apc, orc, cache, dtype, heads, group, d, page):
+    """Calls in tiles of 32 rows hold the weights to 2^-16, however many rows their sequences have."""
+    for sizes in (SMALL, FEW, [(200, 5000), (1, 3000)]):
+        say(f"two parts {dtype} over {cache} heads={heads} group={group} d={d} n={len(sizes)}")
+        made = make_prompt(d + 5, sizes, heads, group, d, page, -(-max(n for _, n in sizes) // page), cache, dtype, pad=3)
+        assert plan_of(made, cache).rows == 32
+        check(orc, cache, dtype, made, d ** -0.5, run_prompt(apc, *made, d ** -0.5))
+
+
 STARTS = {"cut": [-4, 37, 60, 60, 10 ** 6, 10 ** 6 + 5, 2 ** 31 - 1], "falling": [100, 140, 143, 20, 60, 90, -3],
           "turned": [2 ** 31 - 1, 150, 230, 40, 150, 3, -2 ** 31]}
 
