@@ -9,17 +9,19 @@
 namespace apc {
 namespace {
 
-// Joins the parts of units whose keys were cut, in the order of the parts: a
-// workgroup takes ROWS rows of a unit at a time, and the threads of a row stand over
-// (some of the parts) x (elements).
+// Joins the parts of units whose keys were cut: a workgroup takes ROWS rows of a
+// unit at a time.  The threads of a row first go over its parts' maxima and sums of
+// weights, then, as (some of the parts) x (elements), sum the parts' means, each times its
+// share of all weights: a mean at no point outside the values' range.  The order of
+// the sums follows from the number of parts alone.
 template <int DT, int DP, int ROWS>
 __global__ __launch_bounds__(256) void k_prompt_join(apc_kv c, PromptArgs a, PromptPlan p, int kt)
 {
     using T = typename Elem<DT>::T;
-    constexpr int LANES = DP / 4, PER = 256 / ROWS, AT_ONCE = PER / LANES, AHEAD = 4;
+    constexpr int LANES = DP / 4, PER = 256 / ROWS, AT_ONCE = PER / LANES, AHEAD = 4, W = PER < 64 ? PER : 64;
     static_assert(AT_ONCE >= 1);
     __shared__ float acc[ROWS][AT_ONCE][DP];
-    __shared__ float sums[ROWS][AT_ONCE], tops[ROWS][AT_ONCE];
+    __shared__ float tops[PER / W], sums[PER / W];              // of waves that share a row
     const int head = blockIdx.x % c.heads, k = blockIdx.x / c.heads, group = a.q_heads / c.heads;
     const PromptUnit u = prompt_unit(a, group, p.rows, k);
     if (u.seq < 0) return;
@@ -33,49 +35,63 @@ __global__ __launch_bounds__(256) void k_prompt_join(apc_kv c, PromptArgs a, Pro
     for (int r0 = blockIdx.y * ROWS; r0 < rows; r0 += gridDim.y * ROWS) {
         const int r = r0 + i < rows ? r0 + i : r0;              // (a row past the end: the first one's, not stored)
         const int64_t slot = prompt_slot(p, c.heads, k, head, 0) + r;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        float top = LOWEST, sum = 0.f;
-        for (int q0 = part0; q0 < keys.parts; q0 += AT_ONCE * AHEAD) {
-            f32x4 x[AHEAD];
-            float m[AHEAD], l[AHEAD];
+        f32x4 x[AHEAD];
+        float m[AHEAD], l[AHEAD];
+        auto load = [&](int q0) INLINE {
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                const int q = q0 + j * AT_ONCE < keys.parts ? q0 + j * AT_ONCE : q0;
+                const int q = q0 + j * AT_ONCE < keys.parts ? q0 + j * AT_ONCE : part0 < keys.parts ? part0 : 0;
                 const int64_t at = slot + (int64_t)q * p.rows;
                 x[j] = *reinterpret_cast<const f32x4*>(po + at * DP + d);
                 m[j] = pm[at * 2];
                 l[j] = pm[at * 2 + 1];
             }
+        };
+        load(part0);
+        float top = LOWEST, sum = 0.f;
+        auto add = [&](float m, float l) INLINE {
+            const float y = __builtin_fmaxf(top, m);
+            sum = sum * __builtin_amdgcn_exp2f(top - y) + l * __builtin_amdgcn_exp2f(m - y);
+            top = y;
+        };
+        for (int q = threadIdx.x % PER; q < keys.parts; q += PER) {
+            const int64_t at = (slot + (int64_t)q * p.rows) * 2;
+            add(pm[at], pm[at + 1]);
+        }
+#pragma unroll
+        for (int x = W / 2; x > 0; x /= 2) {
+            const float m = __shfl_xor(top, x, W), l = __shfl_xor(sum, x, W);
+            add(m, l);
+        }
+        top = __shfl(top, 0, W), sum = __shfl(sum, 0, W);       // (the same for all lanes, to the last bit)
+        if constexpr (PER > W) {
+            if (threadIdx.x % W == 0) tops[threadIdx.x / W] = top, sums[threadIdx.x / W] = sum;
+            __syncthreads();
+            top = LOWEST, sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < PER / W; ++w) add(tops[w], sums[w]);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int q0 = part0; q0 < keys.parts; q0 += AT_ONCE * AHEAD) {
+            if (q0 != part0) load(q0);
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 if (q0 + j * AT_ONCE >= keys.parts) break;
-                const float y = __builtin_fmaxf(top, m[j]);
-                const float was = __builtin_amdgcn_exp2f(top - y), is = __builtin_amdgcn_exp2f(m[j] - y);
-                v = v * was + x[j] * is;
-                sum = sum * was + l[j] * is;
-                top = y;
+                v += x[j] * (__builtin_amdgcn_exp2f(m[j] - top) * l[j] * inv);
             }
         }
         if constexpr (AT_ONCE > 1) {
-            if (r0 != (int)blockIdx.y * ROWS) __syncthreads();
+            // (waves that share a row have met since the last row's were read)
+            if (PER <= W && r0 != (int)blockIdx.y * ROWS) __syncthreads();
             *reinterpret_cast<f32x4*>(&acc[i][part0][d]) = v;
-            if (d == 0) sums[i][part0] = sum, tops[i][part0] = top;
             __syncthreads();
-#pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) top = __builtin_fmaxf(top, tops[i][j]);
-            sum = 0.f;
             v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) {
-                const float f = __builtin_amdgcn_exp2f(tops[i][j] - top);
-                sum = __builtin_fmaf(f, sums[i][j], sum);
-                v += f * *reinterpret_cast<const f32x4*>(&acc[i][j][d]);
-            }
+            for (int j = 0; j < AT_ONCE; ++j) v += *reinterpret_cast<const f32x4*>(&acc[i][j][d]);
         }
         if (r0 + i < rows && part0 == 0) {
-            const float f = sum == 0.f ? 0.f : 1.0f / sum;
-            const float out[4] = {sum == 0.f ? 0.f : v.x * f, sum == 0.f ? 0.f : v.y * f, sum == 0.f ? 0.f : v.z * f,
-                                  sum == 0.f ? 0.f : v.w * f};
+            const float out[4] = {v.x, v.y, v.z, v.w};
             const int row = u.tile * p.rows + r, h = head * group + row % group;
             const int64_t token = u.first + row / group;
             if (d < c.d) store_values<DT, 4>(static_cast<T*>(a.out) + token * a.out_row + h * a.out_head + d, out);

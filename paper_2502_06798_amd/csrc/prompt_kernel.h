@@ -170,7 +170,8 @@ struct PromptKeys {
     }
 };
 
-// partial results in the workspace: sums (float32, padded d a row), then each row's maximum and sum of weights
+// partial results in the workspace: means (float32, padded d a row), then each row's maximum and sum of weights.  (Means, as
+// sums of values near the end of float32's range would leave it.)
 __host__ __device__ inline int64_t prompt_slots(const PromptPlan& p, int heads) { return (int64_t)p.tiles * heads * p.splits * p.rows; }
 __device__ inline int64_t prompt_slot(const PromptPlan& p, int heads, int k, int head, int part)
 {
@@ -228,7 +229,8 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     const int lo_a = sight.first(pa), lo_z = sight.first(pz), hi_a = sight.end(pa), hi_z = sight.end(pz);
     const int row = row0 + col < all ? row0 + col : all - 1;
     const int token = row / group, qh = head * group + row % group;
-    const int at = sight.past + token, lo = sight.first(at), hi = sight.end(at);
+    const int at = sight.past + token, hi = sight.end(at);
+    int lo = sight.first(at);
     float slope = a.slopes ? a.slopes[qh] : 0.f;
     // (finite where the slope is: no distance times it is 0)
     slope = __builtin_fabsf(slope) > 2.3e38f && __builtin_fabsf(slope) < INFINITY ? __builtin_copysignf(3.4e38f, slope) : slope * LOG2E;
@@ -341,6 +343,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         }
     };
 
+    const int many = PBF ? 32 - __builtin_clz(keys.tiles * KT | 1) : 0;             // (f16 values are far from that range's end)
     f32x16 o[DP / 32];
     float m, l;                                                 // the maximum less OFF, the lane's share of the sum
     auto clear = [&]() INLINE {
@@ -352,7 +355,8 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     };
     // The tile of keys j0 on, at `from` in LDS, into o, m and l.
     // CAREFUL: right for infinite and NaN values, which a weight of 0 makes NaN, and
-    // near the end of float32's range, where weights must not pass 1.
+    // near the end of float32's range, where weights must not pass 1 in all: each is
+    // multiplied by 2^-many, a power of two above the number of keys.
     auto add_tile = [&](auto care, int j0, int32_t pages, const uint16_t* from) INLINE {
         constexpr bool CAREFUL = decltype(care)::value;
         const uint16_t *kk = from, *vv = from + KT * KS;
@@ -509,9 +513,11 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         // weights, of 16 keys at a time, and their values: columns of the keys whose weights the lane has
         u32x4 hi8[KT / 16], lo8[TWO ? KT / 16 : 1], any8[CAREFUL ? KT / 16 : 1];
         float l1 = 0.f;
+        const float down = __uint_as_float((uint32_t)(127 - many) << 23);               // 2^-many
         auto weigh = [&](int x, int i) INLINE {                 // keys 2 i and 2 i + 1 of the lane's eight
             const float s0 = s[x / 2][x % 2 * 8 + 2 * i], s1 = s[x / 2][x % 2 * 8 + 2 * i + 1];
             float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s0, f, -less)), w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s1, f, -less));
+            if constexpr (CAREFUL && PBF) w0 *= down, w1 *= down;
             l += w0, (SHARED ? l1 : l) += w1;                     // (two sums wait less, where there is a register)
             f32x2 y = {1.f, 1.f};
             if constexpr (E8) y = *reinterpret_cast<const f32x2*>(scales + KT + x * 16 + i / 2 * 8 + i % 2 * 2 + 4 * half);
@@ -601,6 +607,12 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[b][i], 0.f, z);
         return z != 0.f;
     };
+    // (else a register holds `lo` through the other loop, for this one alone)
+    auto again = [&]() INLINE {
+        int x = at;
+        asm("" : "+v"(x));
+        lo = sight.first(x);
+    };
     // LDS that only this wave writes and reads needs no barrier, but the order kept
     auto settle = [&]() INLINE {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -610,6 +622,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     const int t0 = keys.tile0 + (int)((int64_t)keys.tiles * part / keys.parts);
     const int t1 = keys.tile0 + (int)((int64_t)keys.tiles * (part + 1) / keys.parts);
     clear();
+    int up = 0;                                                 // what takes 2^-many back, of the sum of weights
     Tile next;
     if constexpr (SHARED) {
         int32_t pg = 0, pn = 0;
@@ -633,6 +646,8 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         }
         if (__builtin_expect(__syncthreads_or(not_finite_out()), 0)) {
             clear();
+            up = many;
+            again();
             for (int t = t0; t < t1; ++t) {
                 pg = find(t * KT);
                 load(next, t * KT, pg);
@@ -663,6 +678,8 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         }
         if (__builtin_expect(__any(not_finite_out()), 0)) {
             clear();
+            up = many;
+            again();
             for (t = t0 + wave; t < t1; t += KW) {
                 pg = find(t * KT);
                 load(next, t * KT, pg);
@@ -674,27 +691,28 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         }
     }
 
-    // results: the rows' own, or their part of them
+    // results: the rows' own means, or those over a part of their keys
     const int64_t slot = prompt_slot(p, c.heads, k, head, part);
-    float* const sums = static_cast<float*>(a.ws);
-    float* const stats = sums + prompt_slots(p, c.heads) * DP;
+    float* const means = static_cast<float*>(a.ws);
+    float* const stats = means + prompt_slots(p, c.heads) * DP;
     l = both_halves_sum(l);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    l = __builtin_amdgcn_ldexpf(l, up);
     if constexpr (SHARED) {
         const bool store = row0 + col < all;
         if (keys.parts > 1) {
-            float* const to = sums + (slot + wave * 32 + col) * DP + 4 * half;
+            float* const to = means + (slot + wave * 32 + col) * DP + 4 * half;
 #pragma unroll
             for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
-                    if (store) *reinterpret_cast<f32x4*>(to + b * 32 + 2 * i) = f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+                    if (store) *reinterpret_cast<f32x4*>(to + b * 32 + 2 * i) = inv * f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
             if (store && half == 0) {
                 stats[(slot + wave * 32 + col) * 2] = m;
                 stats[(slot + wave * 32 + col) * 2 + 1] = l;
             }
             return;
         }
-        const float f = l == 0.f ? 0.f : 1.0f / l;
         T* const to = static_cast<T*>(a.out) + (u.first + token) * a.out_row + qh * a.out_head + 4 * half;
 #pragma unroll
         for (int b = 0; b < DP / 32; ++b)
@@ -702,7 +720,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             for (int i = 0; i < 16; i += 4) {
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[b][i + e] * f;
+                for (int e = 0; e < 4; ++e) v[e] = o[b][i + e] * inv;
                 if (store && b * 32 + 2 * i < c.d) store_values<DT, 4>(to + b * 32 + 2 * i, v);
             }
         if (a.lse && store && half == 0)
@@ -717,37 +735,37 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
                 *reinterpret_cast<f32x4*>(part_o + (wave * 32 + col) * (DP + 4) + b * 32 + 2 * i + 4 * half) =
-                    f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+                    inv * f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
         if (half == 0) part_m[(wave * 32 + col) * 2] = m, part_m[(wave * 32 + col) * 2 + 1] = l;
         __syncthreads();
         constexpr int PER = 64 * KW / 32, OWN = DP / PER;       // threads of a row, elements of a thread
         const int r = threadIdx.x / PER, d0 = threadIdx.x % PER * OWN, mine = u.tile * M + r;
-        float top = LOWEST, sum = 0.f, v[OWN] = {};
+        float top = LOWEST, sum = 0.f, of[KW], v[OWN] = {};
 #pragma unroll
         for (int w = 0; w < KW; ++w) top = __builtin_fmaxf(top, part_m[(w * 32 + r) * 2]);
 #pragma unroll
         for (int w = 0; w < KW; ++w) {
-            const float f = __builtin_amdgcn_exp2f(part_m[(w * 32 + r) * 2] - top);
-            sum = __builtin_fmaf(f, part_m[(w * 32 + r) * 2 + 1], sum);
-#pragma unroll
-            for (int i = 0; i < OWN; ++i) v[i] = __builtin_fmaf(f, part_o[(w * 32 + r) * (DP + 4) + d0 + i], v[i]);
+            of[w] = __builtin_amdgcn_exp2f(part_m[(w * 32 + r) * 2] - top) * part_m[(w * 32 + r) * 2 + 1];
+            sum += of[w];
         }
+        const float f = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+        for (int w = 0; w < KW; ++w)
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) v[i] = __builtin_fmaf(of[w] * f, part_o[(w * 32 + r) * (DP + 4) + d0 + i], v[i]);
         if (mine >= all) return;
         if (keys.parts > 1) {
 #pragma unroll
             for (int i = 0; i < OWN; i += 4)
-                *reinterpret_cast<f32x4*>(sums + (slot + r) * DP + d0 + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+                *reinterpret_cast<f32x4*>(means + (slot + r) * DP + d0 + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
             if (d0 == 0) stats[(slot + r) * 2] = top, stats[(slot + r) * 2 + 1] = sum;
             return;
         }
-        const float f = sum == 0.f ? 0.f : 1.0f / sum;
         int by = group;
         asm("" : "+s"(by));                                     // (else its inverse is held in a register through the loop)
         const int tok = mine / by, h = head * group + mine % by;
         T* const to = static_cast<T*>(a.out) + (u.first + tok) * a.out_row + h * a.out_head + d0;
         constexpr int ST = OWN < 16 ? OWN : 16;                 // d is a multiple of 16
-#pragma unroll
-        for (int i = 0; i < OWN; ++i) v[i] = sum == 0.f ? 0.f : v[i] * f;
 #pragma unroll
         for (int i = 0; i < OWN; i += ST)
             if (d0 + i < c.d) store_values<DT, ST>(to + i, v + i);

@@ -63,7 +63,10 @@ def check(orc, cache, dtype, made, scale, got, heads=None, **kw):
     g, gl = f64(out), f64(lse)
     none = np.isnan(rl)                                      # rows of no sequence
     assert (g[none] == 7).all() and (gl[none] == 7).all()
-    bad = ~(np.abs(g - ro) <= tol) & ~none[..., None]
+    # infinity is a right rounding of what is half a step below the type's last value, or more, and within the tolerance
+    end = {"f16": 65520.0, "bf16": (2.0 - 2.0 ** -8) * 2.0 ** 127}[dtype]
+    over = np.isinf(g) & (np.sign(g) == np.sign(ro)) & (np.abs(ro) + tol >= end)
+    bad = ~(np.abs(g - ro) <= tol) & ~none[..., None] & ~over
     assert not bad.any(), (np.argwhere(bad)[:4], bad.sum(), np.abs(g - ro)[bad].max())
     empty = np.isneginf(rl)
     assert np.array_equal(np.isneginf(gl), empty) and (g[empty] == 0).all()
@@ -455,3 +458,44 @@ def test_tiles_offsets_past_32_bits(apc, orc):
     small = [torch.stack([x[1098], x[0], x[1099]]) for x in (k, v)]
     at = torch.tensor([[0, 1], [1, 2]], dtype=torch.int32, device="cuda")
     check(orc, "bf16", "bf16", ((small[0], small[1], None, None), at, q, starts, lens), d ** -0.5, (out, lse), heads=[0, 7])
+
+
+# (sizes, heads, rows of a tile, parts of the keys) with pages of 64 tokens
+FORMS = {"32 rows": ([(40, 300), (70, 100), (1, 129)], 2, 32, 1), "32 rows, cut": ([(1, 5000), (20, 2100)], 1, 32, 9),
+         "128 rows": (SOME, 52, 128, 1), "128 rows, cut": (CUT, 128, 128, 2)}
+
+
+def make_form(form, seed, group, d, cache, dtype, spread=1.0):
+    sizes, heads, rows, splits = FORMS[form]
+    made = make_prompt(seed, sizes, heads, group, d, 64, -(-max(n for _, n in sizes) // 64), cache, dtype, spread)
+    p = plan_of(made, cache)
+    assert (p.rows, p.splits) == (rows, splits), (p.rows, p.splits)
+    return made, [h for h in (0, 30, 127) if h < heads]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_means_at_the_end_of_the_range(apc, orc, cache, form, d):
+    """bf16 and scaled e4m3 values up to 3.36e38, all of a column of one sign, with like and unlike weights: their mean, not
+    the sum's infinity; and huge values so far apart that each wave's, or each part's, sum is finite and not all of them."""
+    made, heads = make_form(form, 73, 1, d, cache, "bf16")
+    pool, table, q, starts, lens = made
+    g, v = gen(9), pool[1]
+    sign = torch.randint(0, 2, (d,), device="cuda", generator=g) * 2.0 - 1.0
+    size = 0.5 + 0.49 * torch.rand(v.shape, device="cuda", generator=g)
+    if cache == "e4m3":
+        v.copy_(sign * size * 448.0)
+        pool[3].fill_(3.39e38 / 448.0)
+    else:
+        v.copy_(sign * size * 3.39e38)
+    for scale in (0.0, 0.125):
+        say(f"range end {cache} {form} d={d} scale={scale}")
+        check(orc, cache, "bf16", made, scale, run_prompt(apc, *made, scale), heads=heads)
+    say(f"range end {cache} {form} d={d} apart")
+    far = 32 if form == "32 rows" else 512 if form == "32 rows, cut" else 40 if form == "128 rows" else 1040
+    for i, (_, n) in enumerate(FORMS[form][0]):
+        j = torch.arange(n, device="cuda")
+        j = j[j % far != 0]
+        v.view(torch.uint8 if cache == "e4m3" else torch.int16)[table[i][j // 64].long(), :, j % 64] = 0
+    check(orc, cache, "bf16", made, 0.0, run_prompt(apc, *made, 0.0), heads=heads)
