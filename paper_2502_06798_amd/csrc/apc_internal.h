@@ -117,6 +117,8 @@ struct PromptPlan {
     int32_t unit_rows;   // rows of a unit, on the average
     int32_t min_tiles;   // tiles of keys of a part, at least
     float to_cap;        // from products to the tanh's argument
+    int32_t bias;        // scores are lowered by slopes (of 0, where it is only the next)
+    int32_t lift;        // products are taken times 4: the scale in units of log2 is beyond float32's range
 };
 PromptPlan plan_prompt(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages, int32_t window, bool prefix);
 size_t prompt_workspace(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, int32_t max_pages);

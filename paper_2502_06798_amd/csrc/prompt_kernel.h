@@ -449,7 +449,13 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             }
             f = a.cap * LOG2E;
         }
-        if (a.slopes) {
+        if (p.bias) {
+            if (__builtin_expect(p.lift, 0)) {
+#pragma unroll
+                for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] *= 4.f;                        // (a.scale is a fourth of the call's)
+            }
             float away = (float)(at - j0 - 4 * half);           // of the lane's first key; exact where the product matters
             asm volatile("" : "+v"(away));
 #pragma unroll

@@ -12,7 +12,7 @@ DT = {"f16": 1, "bf16": 2, "e4m3": 3}
 
 class Plan(ctypes.Structure):
     _fields_ = ([(f, ctypes.c_int32) for f in ("shift", "dp", "rows", "tiles", "splits", "unit_rows", "min_tiles")] +
-                [("to_cap", ctypes.c_float)])
+                [("to_cap", ctypes.c_float), ("bias", ctypes.c_int32), ("lift", ctypes.c_int32)])
 
 
 def cache(dtype, heads, d, page, n_pages=1000):
@@ -27,7 +27,7 @@ def plan(dtype, t, b, heads, group, d, page, max_pages, window=0, prefix=False):
     f.restype = Plan
     c = cache(dtype, heads, d, page)
     p = f(ctypes.addressof(c), t, b, heads * group, max_pages, window if window < 2 ** 30 else 0, prefix)
-    assert 1 << p.shift == page and p.dp >= d and p.rows in (32, 128) and p.to_cap == 0
+    assert 1 << p.shift == page and p.dp >= d and p.rows in (32, 128) and (p.to_cap, p.bias, p.lift) == (0, 0, 0)
     return p
 
 

@@ -499,3 +499,25 @@ def test_means_at_the_end_of_the_range(apc, orc, cache, form, d):
         j = j[j % far != 0]
         v.view(torch.uint8 if cache == "e4m3" else torch.int16)[table[i][j // 64].long(), :, j % 64] = 0
     check(orc, cache, "bf16", made, 0.0, run_prompt(apc, *made, 0.0), heads=heads)
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("scale", [3e38, -3.4e38])
+def test_scales_at_the_end_of_the_range(apc, orc, cache, dtype, form, scale):
+    """Scales whose product with log2(e) is beyond float32: products of 0 score 0, and tiny ones what they should."""
+    made, heads = make_form(form, 79, 1, 64, cache, dtype)
+    pool, table, q, starts, lens = made
+    say(f"scale {scale} {dtype} over {cache} {form}")
+    p = torch.randint(-2, 3, pool[0].shape[:3], device="cuda", generator=gen(4)).float()
+    q.zero_()
+    pool[0].view(torch.uint8).zero_()
+    # products of p 2^-122, scores of 56 p and more; f16 holds none so small
+    if cache == "e4m3":
+        pool[0][..., 0] = p.to(pool[0].dtype)
+        q[..., 0] = 2.0 ** -10
+        pool[2].fill_(2.0 ** -112)
+    elif cache == "bf16":
+        pool[0][..., 0] = (p * 2.0 ** -61).to(pool[0].dtype)
+        q[..., 0] = 2.0 ** -61
+    check(orc, cache, dtype, made, scale, run_prompt(apc, *made, scale), heads=heads)
