@@ -626,10 +626,12 @@ apc_status apc_attend_prompt_workspace(const apc_kv* c /* host */, int64_t t, in
  * Scores, the running maximum and sum and the output's sums are float32.  The
  * weights of the values enter the matrix product rounded to the type of q (an
  * error of half a step of each weight), or, for f16 over an e4m3 cache, where
- * sequences have few new tokens and in small calls, in two parts (2^-16 of a weight); over f16
- * caches a weight below 2^-25 of its row's heaviest loses bits, and below 2^-36
- * counts as 0; over the others below 2^-126 of it, the end of float32's normal range
- * (over e4m3 times the value's scale as well).
+ * sequences have few new tokens and in small calls, in two parts (2^-16 of a
+ * weight; over f16 caches of those above 2^-21 of their row's heaviest).  Over f16
+ * caches light weights lose no more than that but for 2^-25 of the result, half of
+ * f16's smallest step (where they could, the call takes longer); over the others a weight
+ * below 2^-126 of its row's heaviest, the end of float32's normal range (over e4m3
+ * times its value's scale), counts as 0.
  * dt          type of q and out: the cache's, or APC_F16 / APC_BF16 where the
  *             cache is APC_E4M3.
  * t           rows of q and out; t <= APC_MAX_TOKENS, t * q_heads <= APC_MAX_PROMPT_ROWS.

@@ -40,6 +40,7 @@ namespace apc {
 
 using f32x16 = float __attribute__((ext_vector_type(16)));
 using s16x4 = short __attribute__((ext_vector_type(4)));
+using u16x2 = uint16_t __attribute__((ext_vector_type(2)));
 
 // 32 x 32 x 16: D = A B + C; a lane's 8 values of A are row lane % 32, of B
 // column lane % 32, both at k = 8 (lane / 32); of D column lane % 32, row
@@ -196,6 +197,11 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     constexpr bool PBF = QBF || E8, TWO = !SHARED || PBF != QBF;
     // f16 weights end at 2^-24 and are whole from 2^-14 on: the row's heaviest stands at
     // 2^OFF to 2^15, so weights from 2^-26 of it are whole and those below 2^-36 are left out.
+    // How much more than half a step that costs is bounded on the way (`lack`), and where it
+    // could show in f16 the keys are gone over again with what is left of those weights as
+    // well.  (The bound costs 5% of long prompts with heads of 128, 15% with heads of 64: two
+    // of 8,192, 4 x 8 heads of 128, f16, 1,215 us before and 1,281, with a bias 1,335 and 1,413;
+    // the second products in every tile that holds such weights 2,000, as most do.)
     constexpr float SLACK = PBF ? 8.f : 3.f, OFF = PBF ? 0.f : 12.f;
     constexpr int M = 32 * R, ES = E8 ? 1 : 2;
     constexpr int KT = SHARED && DP <= 128 ? 64 : 32;           // keys of a tile
@@ -229,8 +235,8 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     const int lo_a = sight.first(pa), lo_z = sight.first(pz), hi_a = sight.end(pa), hi_z = sight.end(pz);
     const int row = row0 + col < all ? row0 + col : all - 1;
     const int token = row / group, qh = head * group + row % group;
-    const int at = sight.past + token, hi = sight.end(at);
-    int lo = sight.first(at);
+    int at = sight.past + token, lo = sight.first(at);
+    const int hi = sight.end(at);
     float slope = a.slopes ? a.slopes[qh] : 0.f;
     // (finite where the slope is: no distance times it is 0)
     slope = __builtin_fabsf(slope) > 2.3e38f && __builtin_fabsf(slope) < INFINITY ? __builtin_copysignf(3.4e38f, slope) : slope * LOG2E;
@@ -302,6 +308,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             if ((!SHARED | (wave < 2)) & there(pages, j)) to.scale = (values ? c.v_scale : c.k_scale)[first_row(pages, j)];
         }
     };
+    u16x2 big = {0, 0};                                         // the largest |v| that this thread loads (f16, even and odd ones)
     auto keep = [&](Tile& t, int j0, uint16_t* to) INLINE {
         uint16_t *kk = to, *vv = to + KT * KS;
         if (c.d < DP || j0 + KT > len) {
@@ -331,6 +338,14 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             } else {
                 *reinterpret_cast<u32x4*>(kk + r * KS + ch * 8) = x;
                 *reinterpret_cast<u32x4*>(vv + r * VS + ch * 8) = y;
+                if constexpr (!PBF) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, y[i] & 0x7fff7fffu));
+                    uint32_t z = __builtin_bit_cast(uint32_t, big);
+                    asm volatile("" : "+v"(z) :: "memory");     // (before the next tile's loads, which take these registers)
+                    big = __builtin_bit_cast(u16x2, z);
+                }
             }
         }
         if constexpr (E8) {
@@ -346,6 +361,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     const int many = PBF ? 32 - __builtin_clz(keys.tiles * KT | 1) : 0;             // (f16 values are far from that range's end)
     f32x16 o[DP / 32];
     float m, l;                                                 // the maximum less OFF, the lane's share of the sum
+    float lack = 0.f;                                           // f16 weights' errors beyond half a step: 2^-35 of it at most
     auto clear = [&]() INLINE {
         m = LOWEST, l = 0.f;
 #pragma unroll
@@ -356,7 +372,8 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     // The tile of keys j0 on, at `from` in LDS, into o, m and l.
     // CAREFUL: right for infinite and NaN values, which a weight of 0 makes NaN, and
     // near the end of float32's range, where weights must not pass 1 in all: each is
-    // multiplied by 2^-many, a power of two above the number of keys.
+    // multiplied by 2^-many, a power of two above the number of keys; and for f16
+    // weights however light.
     auto add_tile = [&](auto care, int j0, int32_t pages, const uint16_t* from) INLINE {
         constexpr bool CAREFUL = decltype(care)::value;
         const uint16_t *kk = from, *vv = from + KT * KS;
@@ -415,6 +432,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
                     for (int e = 0; e < 4; ++e) s[b][i + e] *= y[e];
                 }
         }
+        int lacks = 0;
         float f = sc;                                           // s times f: scores in units of log2
         if (a.cap > 0.f) {
             float top = 0.f;
@@ -481,6 +499,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
                 for (int i = g % 2 * 8; i < g % 2 * 8 + 8; ++i) {
                     const uint32_t at = (uint32_t)(g / 2 * 32 + i / 4 * 8 + i % 4 - from);
                     s[g / 2][i] = at < seen ? s[g / 2][i] * by : -INFINITY;
+                    if constexpr (!PBF && !CAREFUL) lacks -= at < seen ? 0 : 1024;      // (as counted below)
                 }
             }
         }
@@ -497,6 +516,7 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             const float y = both_halves_max(__builtin_fmaxf(m, top)), by = __builtin_amdgcn_exp2f(m - y);
             m = y;
             l *= by;
+            if constexpr (!PBF && !CAREFUL) lack *= by;
 #pragma unroll
             for (int b = 0; b < DP / 32; ++b) o[b] *= by;
         }
@@ -515,6 +535,58 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
                     s[b][i] = x > TOP ? TOP : x;
                 }
             f = 1.f, less = 0.f;
+        }
+        const uint16_t* column = vv + (4 * half + (lane & 15) / 4) * VS + (lane >> 4 & 1) * 16 + lane % 4 * 4;
+        auto values_at = [&](int i) INLINE {                    // i: elements 32 (i % (DP / 32)) on of keys 16 (i / (DP / 32)) on
+            const uint16_t* from = column + i / (DP / 32) * 16 * VS + i % (DP / 32) * 32;
+            const uint2 y = read_columns(from), z = read_columns(from + 8 * VS);
+            return u32x4{y.x, y.y, z.x, z.y};
+        };
+        if constexpr (!PBF && CAREFUL) {
+            // What f16 leaves of weights below 2^LIGHT, 2^-25 at most, is taken times 2^39 and added to the sums times 2^39
+            // (below 2^-65 nothing is left there either: 2^-77 of the heaviest, which no f16 result shows).
+            constexpr float LIGHT = TWO ? 0x1p-9f : 0x1p-14f;
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b) o[b] *= 0x1p39f;                          // (exactly: sums are below 2^61)
+            auto add_part = [&](auto which) INLINE {
+                u32x4 w[KT / 16];
+#pragma unroll
+                for (int x = 0; x < KT / 16; ++x)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float z[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            z[e] = s[x / 2][x % 2 * 8 + 2 * i + e];
+                            asm volatile("" : "+v"(z[e]));      // (else the weights below are computed before this)
+                            z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, -less));
+                        }
+                        f32x2 rest = {z[0] < LIGHT ? z[0] : 0.f, z[1] < LIGHT ? z[1] : 0.f};
+#pragma unroll
+                        for (int part = 0; part < (TWO ? 2 : 1); ++part) rest -= unpack<false>(pack<false>(rest.x, rest.y));
+                        rest *= 0x1p39f;
+                        w[x][i] = pack<false>(rest.x, rest.y);
+                        if constexpr (decltype(which)::value) {
+                            rest -= unpack<false>(w[x][i]);
+                            w[x][i] = pack<false>(rest.x, rest.y);
+                        }
+                    }
+#pragma unroll
+                for (int b = 0; b < DP / 32; ++b) {
+#pragma unroll
+                    for (int x = 0; x < KT / 16; ++x) {
+                        u32x4 v = values_at(x * (DP / 32) + b);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] &= ~not_finite<false>(v[e]);
+                        o[b] = mfma32<false>(v, w[x], o[b]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            add_part(std::false_type{});
+            if constexpr (TWO) add_part(std::true_type{});
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b) o[b] *= 0x1p-39f;
         }
         // weights, of 16 keys at a time, and their values: columns of the keys whose weights the lane has
         u32x4 hi8[KT / 16], lo8[TWO ? KT / 16 : 1], any8[CAREFUL ? KT / 16 : 1];
@@ -535,17 +607,16 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
                 w0 *= y.x, w1 *= y.y;
             }
             hi8[x][i] = pack<PBF>(w0, w1);
+            if constexpr (!PBF && !CAREFUL) {
+                // a weight of x 2^-24, x < 1024, is off by at most 2^-25, (1024 - x) 2^-35 more than half a step of it, 2^-35 x
+                const u16x2 less = __builtin_elementwise_sub_sat(u16x2{1024, 1024}, __builtin_bit_cast(u16x2, hi8[x][i]));
+                lacks = (int)__builtin_amdgcn_udot2(less, u16x2{1, 1}, (uint32_t)lacks, false);
+            }
             if constexpr (TWO) {
                 const f32x2 z = unpack<PBF>(hi8[x][i]);
                 lo8[x][i] = pack<PBF>(w0 - z.x, w1 - z.y);
                 if constexpr (CAREFUL) lo8[x][i] &= ~not_finite<PBF>(hi8[x][i]);
             }
-        };
-        const uint16_t* column = vv + (4 * half + (lane & 15) / 4) * VS + (lane >> 4 & 1) * 16 + lane % 4 * 4;
-        auto values_at = [&](int i) INLINE {                    // i: elements 32 (i % (DP / 32)) on of keys 16 (i / (DP / 32)) on
-            const uint16_t* from = column + i / (DP / 32) * 16 * VS + i % (DP / 32) * 32;
-            const uint2 y = read_columns(from), z = read_columns(from + 8 * VS);
-            return u32x4{y.x, y.y, z.x, z.y};
         };
         if constexpr (!CAREFUL) {
             // the next sixteen's weights are computed beside this one's products
@@ -587,16 +658,18 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
                 u32x4 v = values_at(i), out;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) out[e] = v[e] & not_finite<PBF>(v[e]), v[e] &= ~not_finite<PBF>(v[e]);
+                if (__any(out[0] | out[1] | out[2] | out[3])) {
 #pragma unroll 1
-                for (int kind = 0; kind < 3; ++kind) {
-                    u32x4 is;
+                    for (int kind = 0; kind < 3; ++kind) {
+                        u32x4 is;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) is[e] = is_kind<PBF>(out[e], kind);
-                    f32x16 n = {};
-                    n = mfma32<PBF>(is, any8[x], n);
-                    const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+                        for (int e = 0; e < 4; ++e) is[e] = is_kind<PBF>(out[e], kind);
+                        f32x16 n = {};
+                        n = mfma32<PBF>(is, any8[x], n);
+                        const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[b][e] += n[e] > 0.f ? what : 0.f;
+                        for (int e = 0; e < 16; ++e) o[b][e] += n[e] > 0.f ? what : 0.f;
+                    }
                 }
                 o[b] = mfma32<PBF>(v, hi8[x], o[b]);
                 if constexpr (TWO) o[b] = mfma32<PBF>(v, lo8[x], o[b]);
@@ -604,6 +677,9 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
         }
         __builtin_amdgcn_s_setprio(0);
         l += l1;
+        // (of so light keys that they lose all they are, no more than that)
+        if constexpr (!PBF && !CAREFUL)
+            lack += __builtin_fminf((float)lacks, (KT / 2) * __builtin_amdgcn_exp2f(top - m + (OFF + 35.f)));
     };
     auto not_finite_out = [&]() INLINE {
         float z = 0.f;
@@ -613,11 +689,23 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[b][i], 0.f, z);
         return z != 0.f;
     };
-    // (else a register holds `lo` through the other loop, for this one alone)
+    // Whether light weights can be off by more than 2^-25 of f16's mean, half its smallest step: by 2^-35 lack |v| / l
+    auto too_light = [&](float most) INLINE { return both_halves_sum(lack) * most > 1024.f * both_halves_sum(l); };
+    auto largest = [&]() INLINE {                               // |v| that the wave has loaded
+        int x = big.x > big.y ? big.x : big.y;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int y = __shfl_xor(x, d, 64);
+            x = x > y ? x : y;
+        }
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)(x < 0x7bff ? x : 0x7bff));
+    };
+    // (else registers hold these through the other loop, for this one alone)
     auto again = [&]() INLINE {
-        int x = at;
-        asm("" : "+v"(x));
-        lo = sight.first(x);
+        int x = threadIdx.x;
+        asm volatile("" : "+v"(x));
+        x = row0 + (x & 31) < all ? row0 + (x & 31) : all - 1;
+        at = sight.position(x), lo = sight.first(at);
     };
     // LDS that only this wave writes and reads needs no barrier, but the order kept
     auto settle = [&]() INLINE {
@@ -650,7 +738,19 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             here = other, other = x;
             pg = pn, pn = pf;
         }
-        if (__builtin_expect(__syncthreads_or(not_finite_out()), 0)) {
+        bool more = not_finite_out();
+        if constexpr (!PBF) {
+            float* const of = reinterpret_cast<float*>(lds);
+            const float mine = largest();
+            __syncthreads();
+            if (lane == 0) of[wave] = mine;
+            __syncthreads();
+            float most = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) most = __builtin_fmaxf(most, of[r]);
+            more |= too_light(most);
+        }
+        if (__builtin_expect(__syncthreads_or(more), 0)) {
             clear();
             up = many;
             again();
@@ -682,7 +782,9 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
             add_tile(std::false_type{}, t * KT, pg, mine);
             pg = pn, pn = pf;
         }
-        if (__builtin_expect(__any(not_finite_out()), 0)) {
+        bool more = not_finite_out();
+        if constexpr (!PBF) more |= too_light(largest());
+        if (__builtin_expect(__any(more), 0)) {
             clear();
             up = many;
             again();

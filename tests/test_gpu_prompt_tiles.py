@@ -10,6 +10,9 @@ weight is a float32 relative to its row's running maximum, so that 2^-126 of the
 heaviest and less may count as 0, and over e4m3 its product with the value's
 scale is an operand of 16 bits, which may count as 0 below 2^-126 as well: n
 tokens of 2^-126 |v| over the sum of weights (at least 1), and of 2^-126 448.
+Over f16 caches a weight is within half a step however light, but for 2^-25 of
+the result (half of f16's smallest step); in two parts it is within 2^-16 or
+2^-37 of the row's heaviest (half of f16's smallest step, the heaviest at 2^12).
 """
 import numpy as np
 import pytest
@@ -55,11 +58,12 @@ def check(orc, cache, dtype, made, scale, got, heads=None, **kw):
     e = (q.shape[2] + 24) * U * top + cap * 2.0 ** -21
     if slopes is not None:
         e = e + 4 * U * np.abs(slopes).astype(np.float64) * away
-    tol = spread * (4 * e + 2 * (n + 64) * U + (2.0 ** -16 if two else ROUND[dtype]))[..., None]
+    weight = spread * (2.0 ** -16 if two else ROUND[dtype])
+    if cache == "f16":
+        weight = np.minimum(weight + n * 2.0 ** -37 * heavy, spread * ROUND[dtype]) + 2.0 ** -25
+    tol = spread * (4 * e + 2 * (n + 64) * U)[..., None] + weight
     tol = tol + np.abs(ro) * ROUND[dtype] * 1.001 + TINY[dtype]
     tol = tol + n * 2.0 ** -126 * (heavy + (448.0 if cache == "e4m3" else 0.0))
-    if cache == "f16":
-        tol = tol + n * 2.0 ** -37 * heavy
     g, gl = f64(out), f64(lse)
     none = np.isnan(rl)                                      # rows of no sequence
     assert (g[none] == 7).all() and (gl[none] == 7).all()
@@ -521,3 +525,25 @@ def test_scales_at_the_end_of_the_range(apc, orc, cache, dtype, form, scale):
         pool[0][..., 0] = (p * 2.0 ** -61).to(pool[0].dtype)
         q[..., 0] = 2.0 ** -61
     check(orc, cache, dtype, made, scale, run_prompt(apc, *made, scale), heads=heads)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_light_weights_over_f16_keep_their_bits(apc, orc, form, d):
+    """Tokens of 2^-17 to 2^-47 of the heaviest weight, whose value is 0: they are the output, down to f16's last bits."""
+    made, heads = make_form(form, 83, 1, d, "f16", "f16")
+    pool, table, q, starts, lens = made
+    q.zero_()
+    q[:, :, :2] = 1.0
+    pool[1].copy_(pool[1].abs().clamp(max=3.0) * 2.0e4)
+    for gap in (12.0, 15.5, 19.0, 22.0, 25.0, 28.0, 32.0):
+        say(f"light f16 {form} d={d} gap={gap}")
+        pool[0][..., 2:] = 0
+        pool[0][..., 0] = 0
+        pool[0][..., 1].copy_(torch.rand(pool[0].shape[:3], device="cuda", generator=gen(5)))
+        for i in range(len(lens)):
+            for j in (0, 37):
+                heavy = (table[i, 0].item(), slice(None), j)
+                pool[0][heavy][:, 0] = gap
+                pool[1][heavy] = 0
+        check(orc, "f16", "f16", made, 1.0, run_prompt(apc, *made, 1.0), heads=heads)
