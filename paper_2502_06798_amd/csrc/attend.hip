@@ -390,7 +390,9 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
         }
     };
 
-    const float to_log2 = a.scale * LOG2E;
+    // (0 times an infinite factor is no score: then products are taken times 4)
+    const bool lift = __builtin_amdgcn_readfirstlane(__builtin_fabsf(a.scale) > 2.3e38f);
+    const float to_log2 = (lift ? 0.25f * a.scale : a.scale) * LOG2E;
     constexpr int PER = 4 / ES;                                 // elements of a dword of values
     // the i-th pair of keys' dwords put together, element by element
     auto pairs = [](u32x4* v, int i, uint32_t y, uint32_t z) INLINE {
@@ -451,6 +453,11 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void k_attend(apc_kv 
             if constexpr (E8) factor[h] *= key.scale[h];
         }
         if (more) load_k(key, next);
+        if (__builtin_expect(lift, 0))
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[n][h] *= 4.f;
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
 #pragma unroll
