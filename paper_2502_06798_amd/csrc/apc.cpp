@@ -881,7 +881,7 @@ apc_status apc_attend_prompt(const apc_kv* c, apc_dtype dt, int64_t t, const voi
     // (positions are below 2^30, and no window beyond all of them differs from none)
     const int32_t within = window < APC_MAX_TOKENS ? window : 0;
     const apc::PromptArgs a{q, out, starts, pages, lengths, prefix, slopes, lse, ws, t, q_row, q_head, out_row, out_head,
-                            ld_pages, b, q_heads, max_pages, within, scale, cap};
+                            ld_pages, b, q_heads, max_pages, within, scale, cap, nullptr};
     hipError_t err = apc::launch_attend_prompt(dt, *c, a, static_cast<hipStream_t>(stream));
     if (err != hipSuccess) return hip_fail(err, "apc_attend_prompt launch");
     return ok();

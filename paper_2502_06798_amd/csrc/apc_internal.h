@@ -107,6 +107,7 @@ struct PromptArgs {
     int64_t t, q_row, q_head, out_row, out_head, ld_pages;
     int32_t b, q_heads, max_pages, window;
     float scale, cap;
+    const int32_t* sums;                            // row tiles of each 256 sequences, or NULL (launch_attend_prompt's)
 };
 struct PromptPlan {
     int32_t shift;       // log2 of the page

@@ -9,6 +9,21 @@
 namespace apc {
 namespace {
 
+// Row tiles of each 256 sequences
+__global__ __launch_bounds__(256) void k_prompt_sums(PromptArgs a, int group, int rows, int32_t* sums)
+{
+    __shared__ int of[4];
+    int first;
+    int64_t x = prompt_tiles(prompt_rows(a, blockIdx.x * 256 + threadIdx.x, first), group, rows);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d, 64);
+    if (threadIdx.x % 64 == 0) of[threadIdx.x / 64] = x < MOST_TILES ? (int)x : MOST_TILES;
+    __syncthreads();
+    // (only starts that overlap give as many as that; sums of 64 such stay in 32 bits)
+    const int all = of[0] + of[1] + of[2] + of[3];
+    if (threadIdx.x == 0) sums[blockIdx.x] = all < MOST_TILES ? all : MOST_TILES;
+}
+
 // Joins the parts of units whose keys were cut: a workgroup takes ROWS rows of a
 // unit at a time.  The threads of a row first go over its parts' maxima and sums of
 // weights, then, as (some of the parts) x (elements), sum the parts' means, each times its
@@ -129,6 +144,11 @@ constexpr int FEW_ROWS = 32, CUS = 256;
 constexpr int FULL = 2 * CUS, MANY = 8 * CUS, LONG_KEYS = 4096;
 constexpr int min_keys(int rows) { return rows == 32 ? 512 : 1024; }
 
+// Every workgroup looks for its unit among all sequences, 256 a step of some 0.7 us: that is the square of their
+// number, and of more than MANY_SEQUENCES a launch of its own sums up their tiles, 256 to a sum.
+constexpr int MANY_SEQUENCES = 1024;
+size_t sums_bytes(int64_t b) { return b > MANY_SEQUENCES ? ((b + 255) / 256 * sizeof(int32_t) + 255) / 256 * 256 : 0; }
+
 int64_t row_tiles(int64_t t, int64_t b, int group, int rows) { return t * group / rows + (b < t ? b : t); }
 int64_t least_tiles(int64_t t, int64_t b, int group, int rows) { return std::max(std::min(b, t), (t * group + rows - 1) / rows); }
 
@@ -169,7 +189,7 @@ size_t prompt_workspace(const apc_kv& c, int64_t t, int32_t b, int32_t q_heads, 
         if (most < 2) continue;
         slots = std::max(slots, std::min(row_tiles(t, b, group, rows) * c.heads * most, full) * rows);
     }
-    return (size_t)slots * (padded(c.d) + 2) * sizeof(float);
+    return sums_bytes(b) + (size_t)slots * (padded(c.d) + 2) * sizeof(float);
 }
 
 hipError_t launch_attend_prompt(int dt, const apc_kv& c, const PromptArgs& args, hipStream_t s)
@@ -178,6 +198,13 @@ hipError_t launch_attend_prompt(int dt, const apc_kv& c, const PromptArgs& args,
     PromptArgs a = args;
     PromptPlan p = plan_prompt(c, a.t, a.b, a.q_heads, a.max_pages, a.window, a.prefix != nullptr);
     if (c.n_pages == 0) a.max_pages = 0;                        // no page to read from
+    if (const size_t bytes = sums_bytes(a.b)) {
+        int32_t* const sums = static_cast<int32_t*>(a.ws);
+        k_prompt_sums<<<dim3((unsigned)((a.b + 255) / 256)), dim3(256), 0, s>>>(a, a.q_heads / c.heads, p.rows, sums);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        a.sums = sums;
+        a.ws = static_cast<char*>(a.ws) + bytes;
+    }
     // (a cap so far away bends nothing; so near, its inverse ends the range)
     if (a.cap > 0x1p100f) a.cap = 0.f;
     if (a.cap > 0.f) p.to_cap = std::min(std::fabs(a.scale) / a.cap, std::numeric_limits<float>::max());

@@ -97,41 +97,81 @@ __device__ inline float tanh_over_x(float z)
 // a row tile of a sequence: the sequence's first row among the new tokens', their number, the tile
 struct PromptUnit { int seq, first, n, tile; };
 
+// new tokens of sequence i from its first row on (starts outside the rows are cut, falling ones have none)
+__device__ INLINE inline int prompt_rows(const PromptArgs& a, int i, int& first)
+{
+    const int t = (int)a.t;
+    int from = 0, to = 0;
+    if (i < a.b) from = a.starts[i], to = a.starts[i + 1];
+    first = from < 0 ? 0 : from < t ? from : t;
+    to = to < 0 ? 0 : to < t ? to : t;
+    return to > first ? to - first : 0;
+}
+__device__ INLINE inline int prompt_tiles(int n, int group, int rows) { return (int)(((int64_t)n * group + rows - 1) / rows); }
+
+// Of 256 entries, a lane four at a distance of 64, the one with the k-th of what they
+// count, k then the place in it; -1 where they have no more than k, which k then is without.
+// found(u, l): it is the u-th of lane l.
+template <typename F> __device__ INLINE inline int entry_with(const int (&count)[4], int& k, F&& found)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        int upto = count[u];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += o;
+        }
+        const int total = __builtin_amdgcn_readlane(upto, 63);
+        if (k < total) {
+            const int l = __builtin_ctzll(__ballot(upto > k));
+            k -= __builtin_amdgcn_readlane(upto - count[u], l);
+            found(u, l);
+            return 64 * u + l;
+        }
+        k -= total;
+    }
+    return -1;
+}
+
 // The k-th of all sequences' row tiles of `rows` rows, found by every wave for
-// itself, 256 sequences a step.  The last tiles of a sequence come first: where
-// tokens see what stands before them, they have most to do.
+// itself, 256 sequences a step; of many sequences (a.sums) first 256 times 256, whose tiles
+// k_prompt_sums has summed.  The last tiles of a sequence come first: where tokens
+// see what stands before them, they have most to do.
+constexpr int MOST_TILES = 1 << 24;                             // a call has fewer
 __device__ INLINE inline PromptUnit prompt_unit(const PromptArgs& a, int group, int rows, int k)
 {
-    const int lane = threadIdx.x & 63, t = (int)a.t;
-    for (int seq0 = 0; seq0 < a.b; seq0 += 256) {
-        int first[4], n[4], tiles[4];
+    const int lane = threadIdx.x & 63;
+    int seq0 = 0, count[4];
+    if (a.sums) {
+        const int blocks = (a.b + 255) / 256;
+        for (int i = 0;; i += 256) {
+            if (i >= blocks) return PromptUnit{-1, 0, 0, 0};
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = seq0 + 64 * u + lane;
-            int from = 0, to = 0;
-            if (i < a.b) from = a.starts[i], to = a.starts[i + 1];
-            from = from < 0 ? 0 : from < t ? from : t;
-            to = to < 0 ? 0 : to < t ? to : t;
-            first[u] = from;
-            n[u] = to > from ? to - from : 0;
-            tiles[u] = (int)(((int64_t)n[u] * group + rows - 1) / rows);
+            for (int u = 0; u < 4; ++u) count[u] = i + 64 * u + lane < blocks ? a.sums[i + 64 * u + lane] : 0;
+            const int x = entry_with(count, k, [](int, int) INLINE {});
+            if (x >= 0) {
+                seq0 = 256 * (i + x);
+                break;
+            }
         }
+    }
+    for (; seq0 < a.b; seq0 += 256) {
+        int first[4], n[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            if (seq0 + 64 * u >= a.b) break;
-            int upto = tiles[u];
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int o = __shfl_up(upto, d, 64);
-                if (lane >= d) upto += o;
-            }
-            const int total = __builtin_amdgcn_readlane(upto, 63);
-            if (k < total) {
-                const int l = __builtin_ctzll(__ballot(upto > k));
-                return PromptUnit{seq0 + 64 * u + l, __builtin_amdgcn_readlane(first[u], l), __builtin_amdgcn_readlane(n[u], l),
-                                  __builtin_amdgcn_readlane(upto, l) - 1 - k};
-            }
-            k -= total;
+            n[u] = prompt_rows(a, seq0 + 64 * u + lane, first[u]);
+            count[u] = prompt_tiles(n[u], group, rows);
+        }
+        PromptUnit unit{0, 0, 0, 0};
+        unit.seq = entry_with(count, k, [&](int u, int l) INLINE {
+            unit.first = __builtin_amdgcn_readlane(first[u], l), unit.n = __builtin_amdgcn_readlane(n[u], l);
+            unit.tile = __builtin_amdgcn_readlane(count[u], l) - 1 - k;
+        });
+        if (unit.seq >= 0) {
+            unit.seq += seq0;
+            return unit;
         }
     }
     return PromptUnit{-1, 0, 0, 0};

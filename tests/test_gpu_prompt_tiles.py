@@ -547,3 +547,53 @@ def test_light_weights_over_f16_keep_their_bits(apc, orc, form, d):
                 pool[0][heavy][:, 0] = gap
                 pool[1][heavy] = 0
         check(orc, "f16", "f16", made, 1.0, run_prompt(apc, *made, 1.0), heads=heads)
+
+
+MANY = {"32 rows": (3000, 3, 2, 32, 1), "128 rows": (1100, 90, 2, 128, 1), "empty": (2500, 0, 1, 32, 9)}
+
+
+@pytest.mark.parametrize("name", MANY)
+@pytest.mark.parametrize("cache,dtype", KINDS)
+def test_many_sequences(apc, orc, cache, dtype, name):
+    """More sequences than are looked through one by one, with rows of all of them, and of few whose keys are cut."""
+    b, most, group, rows, splits = MANY[name]
+    rng = np.random.default_rng(b)
+    new = rng.integers(0, most + 1, b)
+    sizes = [(int(n), int(n) + int(p)) for n, p in zip(new, rng.integers(0, 20, b))]
+    if name == "empty":
+        sizes[1023], sizes[1024], sizes[2499] = (2, 4700), (1, 30), (1, 5000)
+        sizes = [(n, max(n, length if length > 20 else 0)) for n, length in sizes]
+    else:
+        sizes[700], sizes[b - 1] = (140, 150), (33, 40)
+    say(f"many {name} {dtype} over {cache}")
+    # (a pool that sequences share: random pages of it)
+    pool, _, q, starts, lens = make_prompt(87, [(sum(n for n, _ in sizes), 5000)], 1, group, 64, 64, 79, cache, dtype, pad=5)
+    starts = torch.from_numpy(np.concatenate([[0], np.cumsum([n for n, _ in sizes])])).to(torch.int32).cuda()
+    lens = torch.tensor([n for _, n in sizes], dtype=torch.int32, device="cuda")
+    pages = -(-max(n for _, n in sizes) // 64)
+    table = torch.randint(0, pool[0].shape[0], (b, pages), dtype=torch.int32, device="cuda", generator=gen(6))
+    made = pool, table, q, starts, lens
+    p = plan_of(made, cache)
+    assert (p.rows, p.splits) == (rows, splits), (p.rows, p.splits)
+    check(orc, cache, dtype, made, 0.125, run_prompt(apc, *made, 0.125))
+
+
+def test_a_million_sequences(apc):
+    """Their time is not the square of their number, and each is what it is in a small call."""
+    b = 2 ** 20
+    pool, _, q, _, _ = make_prompt(89, [(b, 16 * 1000)], 1, 1, 16, 16, 1000, "bf16", "bf16")
+    table = torch.randint(0, 1000, (b, 1), dtype=torch.int32, device="cuda", generator=gen(6))
+    lens = torch.randint(0, 17, (b,), dtype=torch.int32, device="cuda", generator=gen(7))
+    starts = torch.arange(b + 1, dtype=torch.int32, device="cuda")
+    run_prompt(apc, pool, table[:2000], q[:2000], starts[:2001], lens[:2000], 0.25)
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    say("a million sequences")
+    begin.record()
+    out, lse = run_prompt(apc, pool, table, q, starts, lens, 0.25)
+    end.record()
+    torch.cuda.synchronize()
+    assert begin.elapsed_time(end) < 500.0                   # (ms; each looked through one by one: 4,000)
+    for i in (0, 500_000, b - 700):
+        some = slice(i, i + 700)
+        a, e = run_prompt(apc, pool, table[some], q[some], starts[:701], lens[some], 0.25)
+        assert torch.equal(a, out[some]) and torch.equal(e, lse[some])
