@@ -82,15 +82,15 @@ template <bool BF> __device__ inline uint32_t is_kind(uint32_t w, int kind)
     return (is(lo) ? ONE : 0u) | (is(hi) ? ONE << 16 : 0u);
 }
 
-// tanh(x) / x for |x| <= NEAR from x^2, within 2^-23 (a polynomial fitted to the
-// smallest largest relative error)
+// tanh(x) / x for |x| <= NEAR from x^2, within 2^-24 as computed: the polynomial of
+// smallest largest relative error (2^-27.7), found by Remez's exchange
 constexpr float NEAR = 0.625f;
 __device__ inline float tanh_over_x(float z)
 {
-    float r = __builtin_fmaf(z, -0.0056599868f, 0.020590985f);
-    r = __builtin_fmaf(z, r, -0.053721067f);
-    r = __builtin_fmaf(z, r, 0.13331127f);
-    r = __builtin_fmaf(z, r, -0.3333326f);
+    float r = __builtin_fmaf(z, -0.0057049873f, 0.020639088f);
+    r = __builtin_fmaf(z, r, -0.053739715f);
+    r = __builtin_fmaf(z, r, 0.13331442f);
+    r = __builtin_fmaf(z, r, -0.3333328f);
     return __builtin_fmaf(z, r, 1.0f);
 }
 
