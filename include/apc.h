@@ -602,7 +602,9 @@ apc_status apc_attend_prompt_workspace(const apc_kv* c /* host */, int64_t t, in
 /*
  * Attention of several new tokens of each of b sequences over the sequence's
  * cached tokens, the new ones' keys and values among them (written before):
- * whole prompts, the next piece of them, or single tokens.  The new tokens' rows
+ * whole prompts, the next piece of them, or single tokens (where each sequence
+ * has one and no cap, slopes or prefix are asked for, apc_attend takes less time).
+ * The new tokens' rows
  * stand one sequence after the other, sequence i's from starts[i] to
  * starts[i + 1]; they are its last ones, so that the row starts[i] + r is the
  * token at position p = len - (starts[i + 1] - starts[i]) + r, len = lengths[i]

@@ -133,8 +133,11 @@ int tile_keys(int rows, int dp) { return rows == 32 || dp > 128 ? 32 : 64; }
 // more rows than that on the average, or where tiles of 128, a wave 32 of them,
 // would be fewer than the CUs: a call of little work is the latency of its longest
 // wave's tiles (7 sequences of 1 to 333 tokens over e4m3, 5 x 2 heads of 80: 19 us,
-// 47 in 76 tiles of 128; 256 tokens, 4 x 8 heads of 128: 10.5 and 14; 1,024 tokens behind
-// 64,512, 8 x 4 heads: 1,400 us in 256 tiles of 128, 2,540 in tiles of 32).
+// 47 in 76 tiles of 128; 256 tokens, 4 x 8 heads of 128: 10.5 and 14; 128 behind 4,000, 8 x
+// 4 heads: 33 and 47).  The rule does not see that keys could be cut, and with long keys tiles
+// of 128 would be faster far below as many as the CUs: 256 tokens behind 4,000 50 us and 51,
+// 512 78 and 69, 992 152 and 110; behind 64,512 128 tokens 403 and 201, 512 1,037 and 599,
+// 992 2,043 and 1,159 (1,024 have 256 tiles: 1,190).
 constexpr int FEW_ROWS = 32, CUS = 256;
 // Keys are cut where units are fewer than the workgroups that the chip holds at
 // once (two a CU), into parts whose time is more than the join's.  Row tiles of 32

@@ -22,9 +22,10 @@
 // 32 rows and every KW-th tile each, in an LDS buffer of their own.
 //
 // Bound, for long SHARED units, by the matrix unit and what it waits for: two
-// prompts of 8,192 tokens, 4 x 8 heads of 128, bf16, take 1,170 us, 0.94 PFLOP/s, its unit
-// busy 45% of the time at 1.9 GHz (a large bf16 product reaches 1.58 in a trace, at
-// 93% and 1.72 GHz); loads cost 150 us of it, the copies to LDS 90.  Tried and not
+// prompts of 8,192 tokens, 4 x 8 heads of 128, bf16, take 1,160 to 1,210 us by box, 0.91 to
+// 0.95 PFLOP/s, its unit busy 45% of the time at 1.9 GHz (a large bf16 product reaches 1.44
+// among other calls, 1.58 by its own time in a trace, at 93% and 1.72 GHz); loads cost 150
+// us of it, the copies to LDS 90.  Tried and not
 // kept: 64 rows a wave (half of the LDS reads, but one wave a SIMD: 1,350 us), 8
 // waves to a tile (1,150; short calls 5 to 10% more), with loads two tiles ahead
 // (no less).  Single tokens are bound by memory: 64 of 16,384 to 32,768, e4m3, 625 us,
@@ -233,7 +234,9 @@ __global__ __launch_bounds__(64 * R * KW, DP > 128 ? 1 : 2) void k_attend_prompt
     // loses up to half a step of it, 2^-11 or 2^-8, as much as the output's rounding
     // to the same type, and in sums over many values no more.  A second part, the
     // rounded rest, is taken where the waves share the keys out, whose time is the
-    // keys' and values' loads, and by f16 queries over e4m3, whose outputs are f16.
+    // keys' and values' loads, and by f16 queries over e4m3, whose outputs are f16.  (In
+    // the others as well: two prompts of 8,192 tokens 1,546 us, 1,194 so; over e4m3, 16 of
+    // 300 to 512, 247 and 212.)
     constexpr bool PBF = QBF || E8, TWO = !SHARED || PBF != QBF;
     // f16 weights end at 2^-24 and are whole from 2^-14 on: the row's heaviest stands at
     // 2^OFF to 2^15, so weights from 2^-26 of it are whole and those below 2^-36 are left out.
